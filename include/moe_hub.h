@@ -58,7 +58,7 @@ enum {
     MOE_SCORE_SIGMOID_TOPK = 1  /* sigmoid of each selected logit, divided by their sum */
 };
 
-enum { MOE_OP_ROUTE = 0, MOE_OP_DISPATCH_LAYOUT = 1, MOE_OP_GROUPED_FFN = 2 };
+enum { MOE_OP_ROUTE = 0, MOE_OP_DISPATCH_LAYOUT = 1, MOE_OP_GROUPED_FFN = 2, MOE_OP_LAYER_FEW = 3 /* moe_few.h */ };
 
 enum { MOE_MAX_EXPERTS = 1024, MOE_MAX_TOPK = 32 };
 
@@ -71,7 +71,8 @@ const char *moe_last_error(void);
 /* Bytes of device workspace `op` needs for these sizes (arguments an op does not
  * use are ignored).  ROUTE: N*E fp32 logits (only when logits_opt is NULL).
  * DISPATCH_LAYOUT: per-chunk expert histograms.  GROUPED_FFN: the activation
- * a[M,F] between the two GEMMs plus the tile schedule.  Returns 0 on bad sizes. */
+ * a[M,F] between the two GEMMs plus the tile schedule.  LAYER_FEW (moe_few.h): parts of
+ * the logits, the activation and the dependency counters.  Returns 0 on bad sizes. */
 size_t moe_workspace_bytes(int op, int64_t N, int64_t H, int E, int K, int G, int64_t F, int dtype);
 
 /*

@@ -1,4 +1,4 @@
-"""ctypes binding of ``include/moe_hub.h``: same names, argument marshalling only."""
+"""ctypes binding of ``include/moe_hub.h`` and ``include/moe_few.h``: same names, argument marshalling only."""
 from __future__ import annotations
 
 import ctypes
@@ -15,7 +15,9 @@ _LIB_PATH = os.environ.get("MOE_HUB_LIBRARY") or os.path.join(HERE, "libmoe_hub.
 
 BF16, F32 = 0, 1
 SCORE_SOFTMAX_TOPK, SCORE_SIGMOID_TOPK = 0, 1
-OP_ROUTE, OP_DISPATCH_LAYOUT, OP_GROUPED_FFN = 0, 1, 2
+OP_ROUTE, OP_DISPATCH_LAYOUT, OP_GROUPED_FFN, OP_LAYER_FEW = 0, 1, 2, 3
+Q4_FP4, Q4_INT4 = 0, 1
+FEW_TOKENS = 64
 
 _ERR_NAMES = {-1: "MOE_ERR_ARG", -2: "MOE_ERR_UNSUPPORTED", -3: "MOE_ERR_WORKSPACE", -4: "MOE_ERR_LAUNCH",
               -5: "MOE_ERR_STATE"}
@@ -54,6 +56,19 @@ _SIGNATURES = {
     "moe_combine": (_c_int, [_c_vp, _c_int, _c_i64, _c_i64, _c_int, _c_vp, _c_vp, _c_vp, _c_vp]),
 }
 
+# the declarations of include/moe_few.h
+_FEW_SIGNATURES = {
+    "moe_layer_few": (_c_int, [_c_vp, _c_int, _c_i64, _c_i64, _c_vp, _c_vp, _c_int, _c_int, _c_int, _c_i64, _c_vp, _c_vp,
+                               _c_vp, _c_vp, _c_vp, _c_vp, _c_vp, _c_sz, _c_vp]),
+    "moe_layer_few_q4": (_c_int, [_c_vp, _c_int, _c_i64, _c_i64, _c_vp, _c_vp, _c_int, _c_int, _c_int, _c_i64, _c_int,
+                                  _c_int, _c_vp, _c_vp, _c_vp, _c_vp, _c_vp, _c_vp, _c_vp, _c_vp, _c_vp, _c_vp, _c_sz,
+                                  _c_vp]),
+    "moe_matvec_q4": (_c_int, [_c_vp, _c_int, _c_i64, _c_i64, _c_i64, _c_int, _c_vp, _c_int, _c_int, _c_vp, _c_vp, _c_vp,
+                               _c_vp]),
+    "moe_quantize_q4": (_c_int, [_c_vp, _c_int, _c_i64, _c_i64, _c_int, _c_int, _c_vp, _c_vp, _c_vp]),
+    "moe_dequantize_q4": (_c_int, [_c_vp, _c_vp, _c_int, _c_int, _c_i64, _c_i64, _c_vp, _c_int, _c_vp]),
+}
+
 _lib = None
 
 
@@ -68,7 +83,13 @@ def lib_path() -> str:
 
 
 def exported_symbols():
+    """The functions of moe_hub.h."""
     return sorted(_SIGNATURES)
+
+
+def exported_few_symbols():
+    """The functions of moe_few.h."""
+    return sorted(_FEW_SIGNATURES)
 
 
 def load_library(build_if_missing: bool = True):
@@ -82,7 +103,7 @@ def load_library(build_if_missing: bool = True):
         from . import build as _build
         _build.build(verbose=False)
     lib = ctypes.CDLL(_LIB_PATH)
-    for name, (res, args) in _SIGNATURES.items():
+    for name, (res, args) in (*_SIGNATURES.items(), *_FEW_SIGNATURES.items()):
         fn = getattr(lib, name)          # AttributeError if a declared symbol is missing
         fn.restype, fn.argtypes = res, args
     _lib = lib
@@ -336,3 +357,104 @@ def moe_combine(y, K: int, slot_of_row, topk_w, out):
     lib = _lib or load_library()
     _check(lib.moe_combine(y.data_ptr(), _dtype_code(y), N, H, K, slot_of_row.data_ptr(), topk_w.data_ptr(),
                            out.data_ptr(), _stream()))
+
+
+# ---- the decoding operators (moe_few.h) ----
+def _need_shape(t, dtype, shape, name):
+    """A contiguous tensor of this type and shape on the current device, whose stream the call goes to."""
+    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous device tensor of {dtype} and shape {shape}")
+    if t.device.index != torch.cuda.current_device():
+        raise TypeError(f"{name} is on another device than the current one")
+
+
+def _need_q4(codes, scales, rows_shape, cols, fmt, group, name):
+    if fmt not in (Q4_FP4, Q4_INT4) or group not in (32, 64, 128):
+        raise ValueError(f"format must be Q4_FP4 or Q4_INT4 and group 32, 64 or 128, got {fmt} and {group}")
+    _need_shape(codes, torch.uint8, (*rows_shape, cols // 2), f"{name} codes")
+    _need_shape(scales, torch.uint8 if fmt == Q4_FP4 else torch.bfloat16, (*rows_shape, -(-cols // group)), f"{name} scales")
+
+
+def _need_layer(x, W_r, bias, K, topk_idx, topk_w, out):
+    if x.dim() != 2 or W_r.dim() != 2:
+        raise TypeError("x and W_r must be matrices")
+    (N, H), E = x.shape, W_r.shape[1]
+    code = _dtype_code(x)
+    _need_shape(x, x.dtype, (N, H), "x")
+    _need_shape(W_r, torch.float32, (H, E), "W_r")
+    if bias is not None:
+        _need_shape(bias, torch.float32, (E,), "bias")
+    _need_shape(topk_idx, torch.int32, (N, K), "topk_idx")
+    _need_shape(topk_w, torch.float32, (N, K), "topk_w")
+    _need_shape(out, x.dtype, (N, H), "out")
+    return N, H, E, code
+
+
+def moe_layer_few(x, W_r, bias, K: int, score_mode: int, W_gate, W_up, W_down, topk_idx, topk_w, out, ws):
+    """The whole layer for at most FEW_TOKENS tokens; ws: workspace_bytes(OP_LAYER_FEW, N, H, E, K, F=F, dtype=...)."""
+    N, H, E, code = _need_layer(x, W_r, bias, K, topk_idx, topk_w, out)
+    F = W_gate.shape[1]
+    _need_shape(W_gate, x.dtype, (E, F, H), "W_gate")
+    _need_shape(W_up, x.dtype, (E, F, H), "W_up")
+    _need_shape(W_down, x.dtype, (E, H, F), "W_down")
+    wp, wb = _ws_args(ws)
+    lib = _lib or load_library()
+    _check(lib.moe_layer_few(x.data_ptr(), code, N, H, W_r.data_ptr(), _ptr(bias), E, K, score_mode, F, W_gate.data_ptr(),
+                             W_up.data_ptr(), W_down.data_ptr(), topk_idx.data_ptr(), topk_w.data_ptr(), out.data_ptr(), wp, wb,
+                             _stream()))
+
+
+def moe_layer_few_q4(x, W_r, bias, K: int, score_mode: int, gate, up, down, fmt: int, group: int, topk_idx, topk_w, out, ws):
+    """moe_layer_few with 4-bit weights: gate, up, down are pairs (codes, scales)."""
+    N, H, E, code = _need_layer(x, W_r, bias, K, topk_idx, topk_w, out)
+    F = gate[0].shape[1]
+    _need_q4(*gate, (E, F), H, fmt, group, "gate")
+    _need_q4(*up, (E, F), H, fmt, group, "up")
+    _need_q4(*down, (E, H), F, fmt, group, "down")
+    wp, wb = _ws_args(ws)
+    lib = _lib or load_library()
+    _check(lib.moe_layer_few_q4(x.data_ptr(), code, N, H, W_r.data_ptr(), _ptr(bias), E, K, score_mode, F, fmt, group,
+                                gate[0].data_ptr(), gate[1].data_ptr(), up[0].data_ptr(), up[1].data_ptr(), down[0].data_ptr(),
+                                down[1].data_ptr(), topk_idx.data_ptr(), topk_w.data_ptr(), out.data_ptr(), wp, wb, _stream()))
+
+
+def moe_matvec_q4(x, seg_offsets, codes, scales, fmt: int, group: int, y):
+    """y[m] = W[e] x[m] for the rows m of expert e's segment; seg_offsets None: one matrix for all rows."""
+    if x.dim() != 2 or codes.dim() != 3:
+        raise TypeError("x must be a matrix and codes a stack of matrices")
+    (M, cols), (E, rows) = x.shape, codes.shape[:2]
+    _need_shape(x, x.dtype, (M, cols), "x")
+    _need_q4(codes, scales, (E, rows), cols, fmt, group, "W")
+    if seg_offsets is not None:
+        _need_shape(seg_offsets, torch.int32, (E + 1,), "seg_offsets")
+    _need_shape(y, x.dtype, (M, rows), "y")
+    lib = _lib or load_library()
+    _check(lib.moe_matvec_q4(x.data_ptr(), _dtype_code(x), M, cols, rows, E, _ptr(seg_offsets), fmt, group, codes.data_ptr(),
+                             scales.data_ptr(), y.data_ptr(), _stream()))
+
+
+def _q4_matrix(w, codes, scales, fmt, group):
+    if w.dim() < 2:
+        raise TypeError("w must be a matrix or a stack of matrices")
+    *lead, cols = w.shape
+    _need_shape(w, w.dtype, tuple(w.shape), "w")
+    _need_q4(codes, scales, tuple(lead), cols, fmt, group, "w's")
+    rows = 1
+    for n in lead:
+        rows *= n
+    return rows, cols
+
+
+def moe_quantize_q4(w, fmt: int, group: int, codes, scales):
+    """w [..., cols] into codes [..., cols / 2] and scales [..., ceil(cols / group)]."""
+    rows, cols = _q4_matrix(w, codes, scales, fmt, group)
+    lib = _lib or load_library()
+    _check(lib.moe_quantize_q4(w.data_ptr(), _dtype_code(w), rows, cols, fmt, group, codes.data_ptr(), scales.data_ptr(),
+                               _stream()))
+
+
+def moe_dequantize_q4(codes, scales, fmt: int, group: int, w):
+    rows, cols = _q4_matrix(w, codes, scales, fmt, group)
+    lib = _lib or load_library()
+    _check(lib.moe_dequantize_q4(codes.data_ptr(), scales.data_ptr(), fmt, group, rows, cols, w.data_ptr(), _dtype_code(w),
+                                 _stream()))

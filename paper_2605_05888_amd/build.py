@@ -17,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmoe_hub.so")
 SOURCES = ["ffn_both.hip", "ffn_both_narrow.hip", "ffn_down_scatter.hip", "ffn_gate_up.hip", "ffn_gate_up_gather.hip", "ffn_down.hip",
-           "ffn_down_narrow.hip", "api.hip", "route.hip", "layout.hip", "rowmove.hip", "ffn.hip", "ffn_f32.hip", "ffn_thin.hip"]
+           "ffn_down_narrow.hip", "api.hip", "route.hip", "layout.hip", "rowmove.hip", "ffn.hip", "ffn_f32.hip", "ffn_thin.hip",
+           "few.hip", "q4.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -87,7 +88,8 @@ def needs_build() -> bool:
         return True
     t = os.path.getmtime(LIB)
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
-    deps.append(os.path.join(os.path.dirname(HERE), "include", "moe_hub.h"))
+    include = os.path.join(os.path.dirname(HERE), "include")
+    deps += [os.path.join(include, f) for f in os.listdir(include)]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

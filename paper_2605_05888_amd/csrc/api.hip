@@ -6,6 +6,8 @@
 #include <string.h>
 
 #include "common.h"
+#include "few.h"
+#include "q4.h"
 
 namespace moe {
 
@@ -108,6 +110,11 @@ extern "C" size_t moe_workspace_bytes(int op, int64_t N, int64_t H, int E, int K
         if (N < 0 || H < 1 || F < 1 || E < 1 || (dtype != MOE_BF16 && dtype != MOE_F32))
             return 0;
         return ffn_workspace_bytes(N, H, F, E, dtype);
+    case MOE_OP_LAYER_FEW:
+        if (N < 0 || N > MOE_FEW_TOKENS || H < 1 || F < 1 || H >= kFewMaxCols || F >= kFewMaxCols || E < 1 ||
+            E > MOE_MAX_EXPERTS || K < 1 || K > MOE_MAX_TOPK || (dtype != MOE_BF16 && dtype != MOE_F32))
+            return 0;
+        return few_workspace_bytes(N, H, E, K, F, dtype);
     default:
         return 0;
     }
@@ -482,4 +489,197 @@ extern "C" int moe_combine(const void *y, int dtype, int64_t N, int64_t H, int K
         return fail(MOE_ERR_ARG, "slot_of_row and topk_w must not be NULL");
     return launch_combine(y, dtype, N, H, K, slot_of_row, topk_w, out,
                           static_cast<hipStream_t>(stream));
+}
+
+// ---- the decoding operators (moe_few.h) ------------------------------------
+namespace moe {
+
+static int check_q4(int format, int group)
+{
+    if (format != MOE_Q4_FP4 && format != MOE_Q4_INT4)
+        return fail(MOE_ERR_ARG, "format %d is neither MOE_Q4_FP4 nor MOE_Q4_INT4", format);
+    if (format == MOE_Q4_FP4 ? group != 32 : (group != 32 && group != 64 && group != 128))
+        return fail(MOE_ERR_UNSUPPORTED, "group must be 32 (MOE_Q4_INT4: 32, 64 or 128) (got %d)", group);
+    return MOE_OK;
+}
+
+static int check_q4_cols(const char *name, int64_t cols)
+{
+    if (cols < 1 || cols >= kFewMaxCols)
+        return fail(MOE_ERR_ARG, "%s must be in [1, 2^22) (got %lld)", name, (long long)cols);
+    if (cols % 64 != 0)
+        return fail(MOE_ERR_UNSUPPORTED, "4-bit weights need %s to be a multiple of 64 (got %lld)", name, (long long)cols);
+    return MOE_OK;
+}
+
+static int check_layer_few(int dtype, int64_t N, int64_t H, int E, int K, int score_mode, int64_t F)
+{
+    MOE_TRY(check_dtype(dtype));
+    MOE_TRY(check_routing_sizes(N, K, E));
+    MOE_TRY(check_rows("H", H, dtype));
+    MOE_TRY(check_rows("F", F, dtype));
+    if (K > MOE_MAX_TOPK)
+        return fail(MOE_ERR_UNSUPPORTED, "K=%d exceeds MOE_MAX_TOPK=%d", K, MOE_MAX_TOPK);
+    if (score_mode != MOE_SCORE_SOFTMAX_TOPK && score_mode != MOE_SCORE_SIGMOID_TOPK)
+        return fail(MOE_ERR_ARG, "unknown score_mode %d", score_mode);
+    if (N > MOE_FEW_TOKENS)
+        return fail(MOE_ERR_UNSUPPORTED, "N=%lld exceeds MOE_FEW_TOKENS=%d", (long long)N, MOE_FEW_TOKENS);
+    if (H >= kFewMaxCols || F >= kFewMaxCols)
+        return fail(MOE_ERR_UNSUPPORTED, "H and F must be below 2^22 (got H=%lld, F=%lld)", (long long)H, (long long)F);
+    if (dtype == MOE_BF16 && (H % 64 != 0 || F % 64 != 0))
+        return fail(MOE_ERR_UNSUPPORTED, "bf16 needs H and F to be multiples of 64 (got H=%lld, F=%lld)", (long long)H,
+                    (long long)F);
+    return MOE_OK;
+}
+
+// Everything but the weights, which the caller has checked.
+static int run_layer_few(const FewArgs &weights, int dtype, int format, const void *x, int64_t N, int64_t H, const float *W_r,
+                         const float *bias, int E, int K, int score_mode, int64_t F, int32_t *topk_idx, float *topk_w, void *out,
+                         void *ws, size_t ws_bytes, void *stream)
+{
+    MOE_NEED(x);
+    MOE_NEED(W_r);
+    MOE_NEED(topk_idx);
+    MOE_NEED(topk_w);
+    MOE_NEED(out);
+    if (bias && !aligned16(bias))
+        return fail(MOE_ERR_ARG, "bias must be 16-byte aligned");
+    const size_t need = few_workspace_bytes(N, H, E, K, F, dtype);
+    if (!ws || ws_bytes < need)
+        return fail(MOE_ERR_WORKSPACE, "the layer needs %zu workspace bytes (got %zu)", need, ws ? ws_bytes : (size_t)0);
+    if (reinterpret_cast<uintptr_t>(ws) % 128 != 0)
+        return fail(MOE_ERR_ARG, "ws must be 128-byte aligned");
+    FewArgs g = weights;
+    g.x = x;
+    g.W_r = W_r;
+    g.bias = bias;
+    g.topk_idx = topk_idx;
+    g.topk_w = topk_w;
+    g.out = out;
+    g.ws = ws;
+    g.N = (int)N;
+    g.H = (int)H;
+    g.E = E;
+    g.K = K;
+    g.F = (int)F;
+    g.score_mode = score_mode;
+    return launch_layer_few(g, dtype, format, static_cast<hipStream_t>(stream));
+}
+
+}  // namespace moe
+
+extern "C" int moe_layer_few(const void *x, int dtype, int64_t N, int64_t H, const float *W_r, const float *bias, int E, int K,
+                             int score_mode, int64_t F, const void *W_gate, const void *W_up, const void *W_down,
+                             int32_t *topk_idx, float *topk_w, void *out, void *ws, size_t ws_bytes, void *stream)
+{
+    clear_error();
+    MOE_TRY(check_layer_few(dtype, N, H, E, K, score_mode, F));
+    if (N == 0)
+        return MOE_OK;
+    MOE_NEED(W_gate);
+    MOE_NEED(W_up);
+    MOE_NEED(W_down);
+    FewArgs g = {};
+    g.gate.data = W_gate;
+    g.up.data = W_up;
+    g.down.data = W_down;
+    return run_layer_few(g, dtype, kNoFormat, x, N, H, W_r, bias, E, K, score_mode, F, topk_idx, topk_w, out, ws, ws_bytes, stream);
+}
+
+extern "C" int moe_layer_few_q4(const void *x, int dtype, int64_t N, int64_t H, const float *W_r, const float *bias, int E, int K,
+                                int score_mode, int64_t F, int format, int group, const void *gate_codes, const void *gate_scales,
+                                const void *up_codes, const void *up_scales, const void *down_codes, const void *down_scales,
+                                int32_t *topk_idx, float *topk_w, void *out, void *ws, size_t ws_bytes, void *stream)
+{
+    clear_error();
+    MOE_TRY(check_q4(format, group));
+    if (dtype == MOE_F32)
+        return fail(MOE_ERR_UNSUPPORTED, "moe_layer_few_q4 is built for MOE_BF16 only");
+    MOE_TRY(check_layer_few(dtype, N, H, E, K, score_mode, F));
+    if (N == 0)
+        return MOE_OK;
+    MOE_NEED(gate_codes);
+    MOE_NEED(gate_scales);
+    MOE_NEED(up_codes);
+    MOE_NEED(up_scales);
+    MOE_NEED(down_codes);
+    MOE_NEED(down_scales);
+    FewArgs g = {};
+    g.gate = {gate_codes, gate_scales};
+    g.up = {up_codes, up_scales};
+    g.down = {down_codes, down_scales};
+    g.group = group;
+    g.scale_cols_h = (int)q4_scale_cols(H, group);
+    g.scale_cols_f = (int)q4_scale_cols(F, group);
+    return run_layer_few(g, dtype, format, x, N, H, W_r, bias, E, K, score_mode, F, topk_idx, topk_w, out, ws, ws_bytes, stream);
+}
+
+extern "C" int moe_matvec_q4(const void *x, int dtype, int64_t M, int64_t cols, int64_t rows, int E_local,
+                             const int32_t *seg_offsets, int format, int group, const void *codes, const void *scales, void *y,
+                             void *stream)
+{
+    clear_error();
+    MOE_TRY(check_dtype(dtype));
+    MOE_TRY(check_q4(format, group));
+    MOE_TRY(check_q4_cols("cols", cols));
+    if (dtype != MOE_BF16)
+        return fail(MOE_ERR_UNSUPPORTED, "moe_matvec_q4 is built for MOE_BF16 only");
+    if (M < 0 || M >= ((int64_t)1 << 31))
+        return fail(MOE_ERR_ARG, "M must be in [0, 2^31) (got %lld)", (long long)M);
+    if (rows < 1 || rows >= ((int64_t)1 << 27))
+        return fail(MOE_ERR_ARG, "rows must be in [1, 2^27) (got %lld)", (long long)rows);
+    MOE_TRY(check_rows("rows", rows, dtype));
+    if (E_local < 1 || E_local > 65535)
+        return fail(MOE_ERR_ARG, "E_local must be in [1, 65535] (got %d)", E_local);
+    if (M == 0)
+        return MOE_OK;
+    if (!seg_offsets && E_local != 1)
+        return fail(MOE_ERR_ARG, "seg_offsets may be NULL only with E_local == 1 (got %d)", E_local);
+    MOE_NEED(x);
+    MOE_NEED(codes);
+    MOE_NEED(scales);
+    MOE_NEED(y);
+    const MatvecArgs g = {x, {codes, scales}, y, seg_offsets, M, rows, (int)cols, group, (int)q4_scale_cols(cols, group)};
+    return launch_matvec_q4(g, E_local, format, static_cast<hipStream_t>(stream));
+}
+
+namespace moe {
+
+static int check_q4_matrix(int dtype, int64_t rows, int64_t cols, int format, int group)
+{
+    MOE_TRY(check_dtype(dtype));
+    MOE_TRY(check_q4(format, group));
+    MOE_TRY(check_q4_cols("cols", cols));
+    if (rows < 0 || rows > ((int64_t)1 << 36) / (cols + group))
+        return fail(MOE_ERR_ARG, "rows must be >= 0 and rows * cols below 2^36 (got rows=%lld, cols=%lld)", (long long)rows,
+                    (long long)cols);
+    return MOE_OK;
+}
+
+}  // namespace moe
+
+extern "C" int moe_quantize_q4(const void *w, int dtype, int64_t rows, int64_t cols, int format, int group, void *codes,
+                               void *scales, void *stream)
+{
+    clear_error();
+    MOE_TRY(check_q4_matrix(dtype, rows, cols, format, group));
+    if (rows == 0)
+        return MOE_OK;
+    MOE_NEED(w);
+    MOE_NEED(codes);
+    MOE_NEED(scales);
+    return launch_quantize_q4(w, dtype, rows, cols, format, group, codes, scales, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int moe_dequantize_q4(const void *codes, const void *scales, int format, int group, int64_t rows, int64_t cols, void *w,
+                                 int dtype, void *stream)
+{
+    clear_error();
+    MOE_TRY(check_q4_matrix(dtype, rows, cols, format, group));
+    if (rows == 0)
+        return MOE_OK;
+    MOE_NEED(codes);
+    MOE_NEED(scales);
+    MOE_NEED(w);
+    return launch_dequantize_q4(codes, scales, format, group, rows, cols, w, dtype, static_cast<hipStream_t>(stream));
 }
