@@ -340,7 +340,7 @@ static int current_device()
     return dev;
 }
 
-static int compute_units()
+int compute_units()
 {
     static std::atomic<int> cus[kMaxDevices];
     const int dev = current_device();
