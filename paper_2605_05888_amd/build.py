@@ -16,7 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmoe_hub.so")
-SOURCES = ["ffn_both.hip", "ffn_both_narrow.hip", "ffn_down_scatter.hip", "ffn_gate_up.hip", "ffn_gate_up_gather.hip", "ffn_down.hip",
+SOURCES = ["few_ffn_int4.hip", "few_ffn_fp4.hip", "few_ffn_f32.hip", "few_ffn_bf16.hip", "ffn_both.hip", "ffn_both_narrow.hip", "ffn_down_scatter.hip", "ffn_gate_up.hip", "ffn_gate_up_gather.hip", "ffn_down.hip",
            "ffn_down_narrow.hip", "api.hip", "route.hip", "layout.hip", "rowmove.hip", "ffn.hip", "ffn_f32.hip", "ffn_thin.hip",
            "few.hip", "q4.hip", "q4_matvec.hip"]
 

@@ -76,19 +76,14 @@ __device__ __forceinline__ Panel panel_of(const FewMatrix &w, int64_t row, int64
     return p;
 }
 
-// Which rows of the activations: `rows` of them, row_of(r) its byte offset from data, all below `bytes`.
-template <class RowOf>
-struct ActRows {
+// Where the activations of a segment are: row r, column c at row_of(r) + c / 16 * tile + c % 16 elements, all below `bytes`.
+// (Row-major matrices: tile is sixteen elements.)
+struct FewActs {
     const unsigned char *data;
     uint32_t bytes;
+    uint32_t tile; // bytes
     int rows;
-    RowOf row_of;
 };
-template <class RowOf>
-__device__ __forceinline__ ActRows<RowOf> act_rows(const void *data, uint32_t bytes, int rows, RowOf row_of)
-{
-    return {static_cast<const unsigned char *>(data), bytes, rows, row_of};
-}
 
 struct FewCols {
     int cols, scale_cols;
@@ -284,68 +279,156 @@ __device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, con
     }
 }
 
-// sums += the products over lines [first, end) of the panels, by one wavefront.
-template <int kForm, int kTT, int kCT, int kDepth, class RowOf>
-__device__ __forceinline__ void few_stream(FewSums<kForm, kTT, kCT> &sums, const Panel (&panel)[kCT], const ActRows<RowOf> &act,
-                                           const FewCols &g, int first, int end)
+// The part of the stream that the next line is fetched from: panels and activations of one segment, for this lane.
+template <int kForm, int kTT, int kCT>
+struct FewCursor {
+    using Form = FewForm<kForm>;
+    static constexpr int kRows = kTT ? kTT : 1, kActs = kTT ? Form::kChunks : 1;
+    Panel panel[kCT];
+    const unsigned char *act;
+    uint32_t act_bytes, act_line; // act_line: bytes from one line's activations to the next one's
+    uint32_t row_off[kRows], chunk_off[kActs];
+    int line, left, lines; // next line, lines left of this wavefront's, lines of a row
+
+    // first column of chunk t of this lane's line
+    static __device__ __forceinline__ int chunk_col(int t)
+    {
+        const int q = threadIdx.x % kWave / 16;
+        return kForm == kFewFp4 ? 32 * q + 8 * t : (Form::kLineCols / Form::kChunks) * t + (16 / Form::kElt) * q;
+    }
+    template <class RowOf>
+    __device__ __forceinline__ void set_acts(const FewActs &a, RowOf row_of)
+    {
+        const int i = threadIdx.x % 16;
+        act = a.data;
+        act_bytes = a.bytes;
+        act_line = (uint32_t)(Form::kLineCols / 16) * a.tile;
+#pragma unroll
+        for (int m = 0; m < kRows; ++m) {
+            const int r = kTT ? 16 * m + i : i / Form::kChunks;
+            row_off[m] = r < a.rows ? row_of(r) : kNowhere;
+        }
+#pragma unroll
+        for (int t = 0; t < kActs; ++t) {
+            const int col = chunk_col(kTT ? t : i % Form::kChunks);
+            chunk_off[t] = (uint32_t)(col / 16) * a.tile + (uint32_t)(col % 16 * Form::kElt);
+        }
+    }
+};
+
+// A wavefront's stream: segment after segment (a panel of weight rows with the activation rows that meet it, some lines of
+// both), without a gap in the loads between them.  The source says what they are:
+//   segments()            how many
+//   length(k)             lines of segment k, at least 1 (lines past the row's end read as zeros)
+//   open(cursor, k)       sets the cursor to segment k; k ascending, kDepth lines ahead of
+//   close(sums, k)        takes the sums of segment k
+//   ready()               called once, when the first weights are under way and before the first activations are asked for;
+//                         false: there are none, the stream ends
+template <int kForm, int kTT, int kCT, int kDepth, class Source>
+__device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
 {
     using Form = FewForm<kForm>;
     using Ops = FewOperands<kForm, kTT, kCT>;
+    using Cursor = FewCursor<kForm, kTT, kCT>;
+    const int segments = source.segments();
+    if (segments == 0) {
+        (void)source.ready();
+        return;
+    }
     const int lane = threadIdx.x % kWave, i = lane % 16, q = lane / 16;
     const uint32_t w_off = (uint32_t)i * (uint32_t)Form::row_bytes(g.cols) + (uint32_t)q * 16u;
-    // first column of chunk t of this lane
-    auto chunk_col = [&](int t) { return kForm == kFewFp4 ? 32 * q + 8 * t : (Form::kLineCols / Form::kChunks) * t + (16 / Form::kElt) * q; };
-    uint32_t a_off[Ops::kRows];
-#pragma unroll
-    for (int m = 0; m < Ops::kRows; ++m) {
-        const int r = kTT ? 16 * m + i : i / Form::kChunks;
-        a_off[m] = r < act.rows ? act.row_of(r) : kNowhere;
-    }
-    const int my_col = chunk_col(i % Form::kChunks); // kTT == 0
+    const int scale_off = i * g.scale_cols;
     const int group_shift = kForm == kFewInt4 ? (g.group == 32 ? 0 : g.group == 64 ? 1 : 2) : 0;
-    auto fetch = [&](Ops &o, int line) {
-        const bool there = line < end; // (lines past the end have no bytes and read as zeros)
+    auto fetch_weights = [&](Ops &o, const Cursor &c) {
+        const bool there = c.line < c.lines; // (else no bytes: zeros, and the number of loads in flight stays)
 #pragma unroll
-        for (int c = 0; c < kCT; ++c) {
-            const auto rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(panel[c].data), 0, there ? (int)panel[c].bytes : 0, 0x00020000);
+        for (int p = 0; p < kCT; ++p) {
+            const auto rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(c.panel[p].data), 0,
+                                                              there ? (int)c.panel[p].bytes : 0, 0x00020000);
 #pragma unroll
             for (int s = 0; s < Form::kLoads; ++s) // (weights are read once: non-temporal)
-                o.w[c][s] = __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(w_off + (uint32_t)(line * Form::kLineBytes + 64 * s)), 0, 2);
+                o.w[p][s] = __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(w_off + (uint32_t)(c.line * Form::kLineBytes + 64 * s)), 0, 2);
             if constexpr (Form::kQ4) {
-                const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(panel[c].scales), 0,
-                                                                  there ? (int)panel[c].scale_bytes : 0, 0x00020000);
-                const int at = i * g.scale_cols + ((line * 4 + q) >> group_shift);
+                const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(c.panel[p].scales), 0,
+                                                                  there ? (int)c.panel[p].scale_bytes : 0, 0x00020000);
+                const int at = scale_off + ((c.line * 4 + q) >> group_shift);
                 if constexpr (kForm == kFewFp4)
-                    o.scale[c] = __builtin_amdgcn_raw_buffer_load_b8(rs, at, 0, 0);
+                    o.scale[p] = __builtin_amdgcn_raw_buffer_load_b8(rs, at, 0, 0);
                 else
-                    o.scale[c] = __builtin_amdgcn_raw_buffer_load_b16(rs, 2 * at, 0, 0);
+                    o.scale[p] = __builtin_amdgcn_raw_buffer_load_b16(rs, 2 * at, 0, 0);
             }
         }
-        const auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(act.data), 0, there ? (int)act.bytes : 0, 0x00020000);
-        auto load_act = [&](int m, int col) { // columns past the row's end would be another row's
-            col += line * Form::kLineCols;
-            const uint32_t at = a_off[m] + (uint32_t)col * Form::kElt;
-            return __builtin_amdgcn_raw_buffer_load_b128(ra, (int)(!Form::kRagged || col < g.cols ? at : kNowhere), 0, 0);
-        };
+    };
+    auto fetch_acts = [&](Ops &o, const Cursor &c) {
+        const bool there = c.line < c.lines;
+        const auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(c.act), 0, there ? (int)c.act_bytes : 0, 0x00020000);
+        const uint32_t base = (uint32_t)c.line * c.act_line;
+        const int col0 = c.line * Form::kLineCols;
 #pragma unroll
-        for (int m = 0; m < Ops::kRows; ++m)
+        for (int t = 0; t < Ops::kActs; ++t) {
+            // columns past the row's end would be another row's
+            const bool in = !Form::kRagged || col0 + Cursor::chunk_col(kTT ? t : i % Form::kChunks) < g.cols;
 #pragma unroll
-            for (int t = 0; t < Ops::kActs; ++t)
-                o.a[m][t] = load_act(m, kTT ? chunk_col(t) : my_col);
+            for (int m = 0; m < Ops::kRows; ++m)
+                o.a[m][t] = __builtin_amdgcn_raw_buffer_load_b128(ra, (int)(in ? c.row_off[m] + c.chunk_off[t] + base : kNowhere), 0, 0);
+        }
+    };
+    Cursor c;
+    int opened = 0; // segments
+    auto open = [&]() {
+        if (opened < segments) {
+            source.open(c, opened);
+            ++opened;
+        } else {
+            c.lines = 0; // nothing more
+            c.left = 0x7FFFFFFF;
+        }
+    };
+    auto advance = [&]() {
+        ++c.line;
+        if (--c.left == 0)
+            open();
         // one order of the loads everywhere: else the wait at the top of the loop is for all of them
         __builtin_amdgcn_sched_barrier(0);
     };
     Ops o[kDepth];
+    {
+        // The weights of the first lines go out before ready(), their activations after it.
+        Cursor starts[kDepth];
+        open();
 #pragma unroll
-    for (int d = 0; d < kDepth; ++d)
-        fetch(o[d], first + d);
-    for (int j = first; j < end; j += kDepth)
+        for (int d = 0; d < kDepth; ++d) {
+            starts[d] = c;
+            fetch_weights(o[d], c);
+            advance();
+        }
+        if (!source.ready())
+            return;
+#pragma unroll
+        for (int d = 0; d < kDepth; ++d)
+            fetch_acts(o[d], starts[d]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    FewSums<kForm, kTT, kCT> sums;
+    sums.clear();
+    int closing = 0, left = source.length(0);
+    for (;;) {
 #pragma unroll
         for (int d = 0; d < kDepth; ++d) {
             few_multiply(sums, o[d], g.group);
             __builtin_amdgcn_sched_barrier(0);
-            fetch(o[d], j + d + kDepth);
+            if (--left == 0) {
+                source.close(sums, closing);
+                if (++closing == segments)
+                    return;
+                sums.clear();
+                left = source.length(closing);
+            }
+            fetch_weights(o[d], c);
+            fetch_acts(o[d], c);
+            advance();
         }
+    }
 }
 
 // LDS and register barrier without the memory fence of __syncthreads, which would wait for the loads in flight.

@@ -9,44 +9,59 @@ constexpr int kMvWaves = 8;
 
 #if defined(__HIP_DEVICE_COMPILE__)
 // Rows [m0, m0 + rows) of x, at most 16 kTT (kTT = 0: 4), with weight rows [n0, n0 + 16 kCT) of matrix e.
-template <int kForm, int kTT, int kCT, int kDepth>
-__device__ __forceinline__ void matvec_tile(const MatvecArgs &g, float *red, int e, int64_t m0, int rows, int64_t n0)
-{
+template <int kForm, int kTT, int kCT>
+struct MatvecTile {
     using Form = FewForm<kForm>;
-    constexpr int kValues = kFewValues<kForm, kTT>;
-    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int64_t row = (int64_t)e * g.rows + n0, end = (int64_t)(e + 1) * g.rows;
-    Panel panels[kCT];
+    const MatvecArgs &g;
+    float *red;
+    int e;
+    int64_t m0;
+    int rows;
+    int64_t n0;
+
+    __device__ __forceinline__ int lines() const { return (g.cols + Form::kLineCols - 1) / Form::kLineCols; }
+    __device__ __forceinline__ int first() const { return lines() * (int)__builtin_amdgcn_readfirstlane(threadIdx.x / kWave) / kMvWaves; }
+    __device__ __forceinline__ int last() const { return lines() * ((int)__builtin_amdgcn_readfirstlane(threadIdx.x / kWave) + 1) / kMvWaves; }
+    __device__ __forceinline__ int segments() const { return 1; }
+    __device__ __forceinline__ int length(int) const { return last() > first() ? last() - first() : 1; }
+    __device__ __forceinline__ bool ready() const { return true; }
+    __device__ __forceinline__ void open(FewCursor<kForm, kTT, kCT> &c, int) const
+    {
+        const int64_t row = (int64_t)e * g.rows + n0, end = (int64_t)(e + 1) * g.rows;
 #pragma unroll
-    for (int c = 0; c < kCT; ++c)
-        panels[c] = panel_of<kForm>(g.w, row + 16 * c, end, g.cols, g.scale_cols);
-    const uint32_t x_row = (uint32_t)g.cols * Form::kElt;
-    const auto act = act_rows(static_cast<const unsigned char *>(g.x) + m0 * x_row, (uint32_t)rows * x_row, rows,
-                              [&](int r) { return r * x_row; });
-    const int lines = (g.cols + Form::kLineCols - 1) / Form::kLineCols;
-    const int first = lines * wave / kMvWaves, last = lines * (wave + 1) / kMvWaves;
-    FewSums<kForm, kTT, kCT> sums;
-    sums.clear();
-    few_stream<kForm, kTT, kCT, kDepth>(sums, panels, act, {g.cols, g.scale_cols, g.group}, first, last);
-#pragma unroll
-    for (int c = 0; c < kCT; ++c)
-#pragma unroll
-        for (int v = 0; v < kValues; ++v)
-            red[((wave * kCT + c) * kValues + v) * kWave + lane] = sums.value(c, v);
-    few_barrier();
-    for (int o = wave; o < kCT * kValues; o += kMvWaves) {
-        float v = red[o * kWave + lane];
-#pragma unroll
-        for (int w = 1; w < kMvWaves; ++w)
-            v += red[(w * kCT * kValues + o) * kWave + lane];
-        const int r = few_row_of<kForm, kTT>(o % kValues);
-        const int64_t n = n0 + 16 * (o / kValues) + lane % 16;
-        const uint32_t both = pack_bf16x2(v, __shfl_xor(v, 1)); // the even lane stores both columns
-        if (r < rows && n < g.rows && lane % 2 == 0)
-            *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(g.y) + (m0 + r) * g.rows + n) = both;
+        for (int p = 0; p < kCT; ++p)
+            c.panel[p] = panel_of<kForm>(g.w, row + 16 * p, end, g.cols, g.scale_cols);
+        const uint32_t x_row = (uint32_t)g.cols * Form::kElt;
+        c.set_acts({static_cast<const unsigned char *>(g.x) + m0 * x_row, (uint32_t)rows * x_row, 16 * Form::kElt, rows},
+                   [&](int r) { return r * x_row; });
+        c.line = last() > first() ? first() : lines(); // (fewer lines than wavefronts: some have none)
+        c.left = length(0);
+        c.lines = lines();
     }
-    few_barrier(); // (red is written again by the next rows)
-}
+    __device__ __forceinline__ void close(const FewSums<kForm, kTT, kCT> &sums, int) const
+    {
+        constexpr int kValues = kFewValues<kForm, kTT>;
+        const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+#pragma unroll
+        for (int c = 0; c < kCT; ++c)
+#pragma unroll
+            for (int v = 0; v < kValues; ++v)
+                red[((wave * kCT + c) * kValues + v) * kWave + lane] = sums.value(c, v);
+        few_barrier();
+        for (int o = wave; o < kCT * kValues; o += kMvWaves) {
+            float v = red[o * kWave + lane];
+#pragma unroll
+            for (int w = 1; w < kMvWaves; ++w)
+                v += red[(w * kCT * kValues + o) * kWave + lane];
+            const int r = few_row_of<kForm, kTT>(o % kValues);
+            const int64_t n = n0 + 16 * (o / kValues) + lane % 16;
+            const uint32_t both = pack_bf16x2(v, __shfl_xor(v, 1)); // the even lane stores both columns
+            if (r < rows && n < g.rows && lane % 2 == 0)
+                *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(g.y) + (m0 + r) * g.rows + n) = both;
+        }
+        few_barrier(); // (red is written again by the next rows)
+    }
+};
 #endif
 
 template <int kForm, int kMaxTT, int kCT>
@@ -59,14 +74,20 @@ __global__ __launch_bounds__(kMvWaves *kWave, kMaxTT == 1 ? 4 : 2) void q4_matve
     const int64_t m1 = g.seg_offsets ? g.seg_offsets[e + 1] : g.M;
     for (int64_t m0 = g.seg_offsets ? g.seg_offsets[e] : 0; m0 < m1; m0 += 16 * kMaxTT) {
         const int rows = (int)(m1 - m0 < 16 * kMaxTT ? m1 - m0 : 16 * kMaxTT);
+        const FewCols cols = {g.cols, g.scale_cols, g.group};
+        auto tile = [&](auto tt, auto depth) {
+            constexpr int kTT = decltype(tt)::value;
+            MatvecTile<kForm, kTT, kCT> t = {g, red, e, m0, rows, n0};
+            few_stream<kForm, kTT, kCT, decltype(depth)::value>(t, cols);
+        };
         if (rows <= FewForm<kForm>::kFewRows)
-            matvec_tile<kForm, 0, kCT, 4>(g, red, e, m0, rows, n0);
+            tile(std::integral_constant<int, 0>{}, std::integral_constant<int, 4>{});
         else if (kMaxTT == 1 || rows <= 16)
-            matvec_tile<kForm, 1, kCT, 3>(g, red, e, m0, rows, n0);
+            tile(std::integral_constant<int, 1>{}, std::integral_constant<int, 3>{});
         else if (rows <= 32)
-            matvec_tile<kForm, (kMaxTT < 2 ? 1 : 2), kCT, 3>(g, red, e, m0, rows, n0);
+            tile(std::integral_constant<int, (kMaxTT < 2 ? 1 : 2)>{}, std::integral_constant<int, 3>{});
         else
-            matvec_tile<kForm, kMaxTT, kCT, 2>(g, red, e, m0, rows, n0);
+            tile(std::integral_constant<int, kMaxTT>{}, std::integral_constant<int, 2>{});
     }
 #endif
 }
