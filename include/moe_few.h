@@ -44,7 +44,7 @@ enum { MOE_FEW_TOKENS = 64 };
  *   ws: moe_workspace_bytes(MOE_OP_LAYER_FEW, N, H, E, K, 0, F, dtype), 128-byte aligned; it needs no
  *   initialisation and may be used for anything else between calls.  Two calls that may overlap
  *   need a workspace each.
- * MOE_BF16: H and F multiples of 64.  MOE_F32: multiples of 4.  H, F below 2^22.
+ * MOE_BF16: H and F multiples of 64.  MOE_F32: multiples of 4.  H, F below 2^21.
  */
 int moe_layer_few(const void *x, int dtype, int64_t N, int64_t H, const float *W_r, const float *bias, int E, int K,
                   int score_mode, int64_t F, const void *W_gate, const void *W_up, const void *W_down,
@@ -68,7 +68,7 @@ int moe_layer_few_q4(const void *x, int dtype, int64_t N, int64_t H, const float
  * (the weights are read once per 64 rows of a segment).  Rows outside every segment are not written.
  *   x [M,cols] dtype   codes [E_local,rows,cols/2]   scales [E_local,rows,ceil(cols/group)]   y [M,rows] dtype (out)
  *   seg_offsets [E_local+1] int32 ON THE DEVICE, non-decreasing, within [0,M]
- * MOE_BF16 only; rows a multiple of 8; cols below 2^22, rows below 2^27; E_local <= 65535.
+ * MOE_BF16 only; rows a multiple of 8; cols below 2^21, rows below 2^27; E_local <= 65535.
  */
 int moe_matvec_q4(const void *x, int dtype, int64_t M, int64_t cols, int64_t rows, int E_local, const int32_t *seg_offsets,
                   int format, int group, const void *codes, const void *scales, void *y, void *stream);

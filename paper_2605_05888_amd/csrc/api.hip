@@ -503,12 +503,12 @@ static int check_q4(int format, int group)
     return MOE_OK;
 }
 
-static int check_q4_cols(const char *name, int64_t cols)
+static int check_q4_cols(int64_t cols, int64_t limit)
 {
-    if (cols < 1 || cols >= kFewMaxCols)
-        return fail(MOE_ERR_ARG, "%s must be in [1, 2^22) (got %lld)", name, (long long)cols);
+    if (cols < 1 || cols >= limit)
+        return fail(MOE_ERR_ARG, "cols must be in [1, %lld) (got %lld)", (long long)limit, (long long)cols);
     if (cols % 64 != 0)
-        return fail(MOE_ERR_UNSUPPORTED, "4-bit weights need %s to be a multiple of 64 (got %lld)", name, (long long)cols);
+        return fail(MOE_ERR_UNSUPPORTED, "4-bit weights need cols to be a multiple of 64 (got %lld)", (long long)cols);
     return MOE_OK;
 }
 
@@ -525,7 +525,7 @@ static int check_layer_few(int dtype, int64_t N, int64_t H, int E, int K, int sc
     if (N > MOE_FEW_TOKENS)
         return fail(MOE_ERR_UNSUPPORTED, "N=%lld exceeds MOE_FEW_TOKENS=%d", (long long)N, MOE_FEW_TOKENS);
     if (H >= kFewMaxCols || F >= kFewMaxCols)
-        return fail(MOE_ERR_UNSUPPORTED, "H and F must be below 2^22 (got H=%lld, F=%lld)", (long long)H, (long long)F);
+        return fail(MOE_ERR_UNSUPPORTED, "H and F must be below 2^21 (got H=%lld, F=%lld)", (long long)H, (long long)F);
     if (dtype == MOE_BF16 && (H % 64 != 0 || F % 64 != 0))
         return fail(MOE_ERR_UNSUPPORTED, "bf16 needs H and F to be multiples of 64 (got H=%lld, F=%lld)", (long long)H,
                     (long long)F);
@@ -621,7 +621,7 @@ extern "C" int moe_matvec_q4(const void *x, int dtype, int64_t M, int64_t cols, 
     clear_error();
     MOE_TRY(check_dtype(dtype));
     MOE_TRY(check_q4(format, group));
-    MOE_TRY(check_q4_cols("cols", cols));
+    MOE_TRY(check_q4_cols(cols, kFewMaxCols));
     if (dtype != MOE_BF16)
         return fail(MOE_ERR_UNSUPPORTED, "moe_matvec_q4 is built for MOE_BF16 only");
     if (M < 0 || M >= ((int64_t)1 << 31))
@@ -649,7 +649,7 @@ static int check_q4_matrix(int dtype, int64_t rows, int64_t cols, int format, in
 {
     MOE_TRY(check_dtype(dtype));
     MOE_TRY(check_q4(format, group));
-    MOE_TRY(check_q4_cols("cols", cols));
+    MOE_TRY(check_q4_cols(cols, (int64_t)1 << 22));
     if (rows < 0 || rows > ((int64_t)1 << 36) / (cols + group))
         return fail(MOE_ERR_ARG, "rows must be >= 0 and rows * cols below 2^36 (got rows=%lld, cols=%lld)", (long long)rows,
                     (long long)cols);

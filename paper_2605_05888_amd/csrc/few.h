@@ -6,7 +6,7 @@
 
 namespace moe {
 
-constexpr int64_t kFewMaxCols = (int64_t)1 << 22; // of H, F and the columns of 4-bit weights
+constexpr int64_t kFewMaxCols = (int64_t)1 << 21; // of H, F and the columns of 4-bit weights
 constexpr int kNoFormat = -1; // weights in the activations' dtype
 
 struct FewMatrix {

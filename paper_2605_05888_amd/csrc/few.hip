@@ -1,4 +1,5 @@
 // The whole layer for a few tokens: router logits and the launches (few_ffn.h has the rest of the layer).
+#include <math.h>
 #include <stdlib.h>
 
 #include "common.h"
@@ -98,17 +99,35 @@ struct FewWorkspace {
 static FewWorkspace few_carve(void *ws, int64_t N, int E, int K, int64_t F, int dtype)
 {
     unsigned char *const w = static_cast<unsigned char *>(ws);
-    const size_t elt = dtype == MOE_BF16 ? 2 : 4, pad = 128 / (16 * elt);
+    const size_t elt = dtype == MOE_BF16 ? 2 : 4;
     const size_t parts = kFlags * sizeof(uint32_t), a = parts + ((size_t)N * kParts * E * sizeof(float) + 127) / 128 * 128;
-    const size_t rows = (size_t)N * K, slots = rows + (pad - 1) * (rows < (size_t)E ? rows : (size_t)E);
+    // tiles of at least 8 columns, each expert's in whole cache lines: at most 15 bytes a column are lost
+    const size_t rows = (size_t)N * K, experts = rows < (size_t)E ? rows : (size_t)E, cols = F + 32;
     return {reinterpret_cast<uint32_t *>(w), reinterpret_cast<float *>(w + parts), w + a,
-            a + (slots * ((F + 15) / 16 * 16) * elt + 127) / 128 * 128};
+            a + rows * cols * elt + experts * cols * 16};
 }
 
 size_t few_workspace_bytes(int64_t N, int64_t H, int E, int K, int64_t F, int dtype)
 {
     (void)H;
     return few_carve(nullptr, N, E, K, F, dtype).bytes;
+}
+
+// Width and split of the gate/up items: the least time of the longest share, in units of a line of one column.  Narrow items
+// make even shares of little work (one token, 4 experts of 1408 columns: 22 columns per workgroup, three items of 8 or two of
+// 16), wide ones use their loads and registers better; a wavefront's lines go in groups of four.
+static void choose_items(FewKernelArgs &g, int widest, int line_cols)
+{
+    const double touched = g.l.E * (1.0 - pow(1.0 - (double)g.l.K / g.l.E, g.l.N)); // experts, if all are equally popular
+    const int64_t experts = touched < 1.0 ? 1 : (int64_t)(touched + 0.5), lines = ceil_div(g.l.H, line_cols);
+    int64_t least = INT64_MAX;
+    for (int width = widest; width >= 8; width -= 8)
+        for (int split = kFewWaves; split >= 1; split /= 2) {
+            const int64_t rounds = ceil_div(ceil_div(experts * ceil_div(g.l.F, width), kFewWaves / split), g.shares);
+            const int64_t time = rounds * (ceil_div(ceil_div(lines, split), 4) * 4 * (width + 4) + 8);
+            if (time < least)
+                least = time, g.width = width, g.split = split;
+        }
 }
 
 int launch_layer_few(const FewArgs &args, int dtype, int format, hipStream_t st)
@@ -124,6 +143,12 @@ int launch_layer_few(const FewArgs &args, int dtype, int format, hipStream_t st)
     // columns of a down tile: as many tiles as workgroups (or a multiple), none wider than 32
     const int64_t rounds = ceil_div(args.H, 32 * (int64_t)g.shares);
     g.down_cols = (int)(ceil_div(ceil_div(args.H, rounds * g.shares), 4) * 4);
+    const int line_cols = format != kNoFormat ? 128 : dtype == MOE_BF16 ? 64 : 32;
+    choose_items(g, format == MOE_Q4_FP4 ? 16 * kGateTiles<kFewFp4> : 16, line_cols);
+    g.h_lines = (int)ceil_div(args.H, line_cols);
+    g.part_lines = (int)ceil_div(g.h_lines, g.split);
+    g.f_tiles = (int)ceil_div(args.F, g.width);
+    g.f_lines = (int)ceil_div(args.F, line_cols);
     const char *const patience = getenv("MOE_FEW_PATIENCE"); // (tests: 0 makes every workgroup take over what is missing)
     g.patience = patience ? atoi(patience) : kDefaultPatience;
     const dim3 grid((unsigned)(ceil_div(args.E, 16) * kParts), (unsigned)ceil_div(args.N, 16));

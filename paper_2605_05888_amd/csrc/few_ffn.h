@@ -41,20 +41,28 @@ constexpr int kMaxRows = MOE_FEW_TOKENS * MOE_MAX_TOPK;
 constexpr int kTokenFlags = MOE_FEW_TOKENS / kFewWaves, kMaxShares = 1024, kFlags = 32 + kMaxShares; // tokens', then shares'
 constexpr int kDefaultPatience = 1 << 15; // polls (about a microsecond each): longer than a share takes
 
-// An expert's rows of the activation are a multiple of this many, so that an item of 16 columns is whole cache lines.
-template <int kForm>
-constexpr int kRowPad = 128 / (16 * FewForm<kForm>::kElt);
-constexpr int kMaxSlots = kMaxRows + 3 * MOE_MAX_EXPERTS;
-
 // ------------------------------------------------------------------------
 struct FewKernelArgs {
     FewArgs l;
     const float *parts;
     uint32_t *flags;
     int shares;    // of gate/up items
+    int width;     // columns of F of an item: a multiple of 8, at most 16 * kGateTiles
+    int split;     // wavefronts that share an item's reduction: 8, 4, 2 or 1
     int down_cols; // columns of H of a down tile, at most 16 kCT
     int patience;
+    int h_lines, part_lines, f_tiles, f_lines; // lines of H, of a wavefront's part of them; items' tiles of F; lines of F
 };
+
+// Sixteens of columns of a gate/up item, each of both matrices.
+template <int kForm>
+constexpr int kGateTiles = kForm == kFewFp4 ? 2 : 1;
+
+// A round's partial sums in LDS (all wavefronts), and how many rounds' there are room for.
+template <int kForm, int kTT>
+constexpr int kRoundFloats = kFewWaves * 2 * kGateTiles<kForm> * (kTT ? 4 * kTT : 4 / FewForm<kForm>::kChunks) * kWave;
+template <int kForm, int kTT>
+constexpr int kRoundsHeld = kRoundFloats<kForm, kTT> > 16384 ? 1 : 2;
 
 #if defined(__HIP_DEVICE_COMPILE__)
 __device__ __forceinline__ float silu_mul_f32(float g, float u) { return g / (1.0f + expf(-g)) * u; }
@@ -85,9 +93,10 @@ __device__ __forceinline__ Pick few_select(const FewKernelArgs &g, int n)
 struct FewLists {
     int begin[5]; // of the classes: at most kFewRows rows, 16, 32, 64
     uint16_t expert[MOE_MAX_EXPERTS], base[MOE_MAX_EXPERTS];
+    uint16_t lines[MOE_MAX_EXPERTS]; // cache lines of one activation tile before this expert's
     uint8_t rows[MOE_MAX_EXPERTS];
-    uint8_t token[kMaxSlots];
-    float weight[kMaxSlots];
+    uint8_t token[kMaxRows];
+    float weight[kMaxRows];
 };
 struct FewRouting { // while the lists are made
     uint64_t mask[MOE_MAX_EXPERTS];  // of tokens
@@ -95,41 +104,58 @@ struct FewRouting { // while the lists are made
     uint16_t pick[kMaxRows];
     float weight[kMaxRows];
     uint64_t wave_sum[kFewWaves];
+    uint32_t wave_rows[kFewWaves];
 };
+
+// An expert's activation: tiles of `width` columns; a tile is its rows side by side, in whole cache lines.
+template <int kForm>
+__device__ __forceinline__ uint32_t few_tile_lines(int rows, int width)
+{
+    return (uint32_t)(rows * width * FewForm<kForm>::kElt + 127) / 128u;
+}
 
 // All threads; r.pick and r.weight are there, r.mask is zero.
 template <int kForm>
-__device__ __forceinline__ void few_make_lists(FewLists &lists, FewRouting &r, int N, int K, int E)
+__device__ __forceinline__ void few_make_lists(FewLists &lists, FewRouting &r, int N, int K, int E, int width)
 {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     for (int at = threadIdx.x; at < N * K; at += kFewThreads)
         atomicOr(reinterpret_cast<unsigned long long *>(&r.mask[r.pick[at]]), 1ull << (at / K));
     __syncthreads();
-    // Two experts per thread.  Sums: slots in the low 13 bits, then experts of each class in 11 bits.
+    // Two experts per thread.  Sums: cache lines of a tile in the low 13 bits, then experts of each class in 11 bits; slots.
     constexpr int kPer = MOE_MAX_EXPERTS / kFewThreads;
     auto shift_of = [](int rows) { return 13 + 11 * (rows <= FewForm<kForm>::kFewRows ? 0 : rows <= 16 ? 1 : rows <= 32 ? 2 : 3); };
-    uint64_t mine[kPer], sum = 0;
+    uint64_t mine[kPer], up_to = 0;
+    uint32_t slots = 0;
     int rows[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int e = threadIdx.x * kPer + i;
         rows[i] = e < E ? (int)__popcll(r.mask[e]) : 0;
-        mine[i] = rows[i] ? (uint64_t)((rows[i] + kRowPad<kForm> - 1) / kRowPad<kForm> * kRowPad<kForm>) | 1ull << shift_of(rows[i]) : 0;
-        sum += mine[i];
+        mine[i] = rows[i] ? (uint64_t)few_tile_lines<kForm>(rows[i], width) | 1ull << shift_of(rows[i]) : 0;
+        up_to += mine[i];
+        slots += rows[i];
     }
-    uint64_t up_to = sum;
+    uint64_t at = 0 - up_to, all = 0;
+    uint32_t slot = 0u - slots;
 #pragma unroll
     for (int s = 1; s < kWave; s <<= 1) {
         const uint64_t v = __shfl_up((unsigned long long)up_to, s);
+        const uint32_t u = __shfl_up(slots, s);
         up_to += lane >= s ? v : 0;
+        slots += lane >= s ? u : 0u;
     }
-    if (lane == kWave - 1)
+    if (lane == kWave - 1) {
         r.wave_sum[wave] = up_to;
+        r.wave_rows[wave] = slots;
+    }
     __syncthreads();
-    uint64_t at = up_to - sum, all = 0;
+    at += up_to;
+    slot += slots;
 #pragma unroll
     for (int w = 0; w < kFewWaves; ++w) {
         at += w < wave ? r.wave_sum[w] : 0;
+        slot += w < wave ? r.wave_rows[w] : 0u;
         all += r.wave_sum[w];
     }
     int begin[5] = {0, 0, 0, 0, 0};
@@ -140,12 +166,14 @@ __device__ __forceinline__ void few_make_lists(FewLists &lists, FewRouting &r, i
     for (int i = 0; i < kPer; ++i) {
         if (rows[i]) {
             const int e = threadIdx.x * kPer + i, shift = shift_of(rows[i]);
-            const int place = begin[(shift - 13) / 11] + (int)(at >> shift & 0x7FF);
+            const int place = (shift == 13 ? 0 : shift == 24 ? begin[1] : shift == 35 ? begin[2] : begin[3]) + (int)(at >> shift & 0x7FF);
             lists.expert[place] = (uint16_t)e;
             lists.rows[place] = (uint8_t)rows[i];
-            lists.base[place] = r.first[e] = (uint16_t)(at & 0x1FFF);
+            lists.lines[place] = (uint16_t)(at & 0x1FFF);
+            lists.base[place] = r.first[e] = (uint16_t)slot;
         }
         at += mine[i];
+        slot += rows[i];
     }
     if (threadIdx.x == 0)
 #pragma unroll
@@ -154,9 +182,9 @@ __device__ __forceinline__ void few_make_lists(FewLists &lists, FewRouting &r, i
     __syncthreads();
     for (int p = threadIdx.x; p < N * K; p += kFewThreads) {
         const int e = r.pick[p], n = p / K;
-        const int slot = r.first[e] + (int)__popcll(r.mask[e] & ((1ull << n) - 1));
-        lists.token[slot] = (uint8_t)n;
-        lists.weight[slot] = r.weight[p];
+        const int s = r.first[e] + (int)__popcll(r.mask[e] & ((1ull << n) - 1));
+        lists.token[s] = (uint8_t)n;
+        lists.weight[s] = r.weight[p];
     }
     __syncthreads();
 }
@@ -202,111 +230,116 @@ __device__ __forceinline__ void few_signal(uint32_t *flag)
 template <int kForm, int kTT, int kCT>
 constexpr int few_depth()
 {
-    if (kForm == kFewInt4)
-        return kTT == 0 ? 6 : kTT == 1 ? 4 : 2;
-    if (FewForm<kForm>::kQ4) // 5 kCT + 4, 16, 32, 64
-        return kTT == 0 ? 8 : kTT == 1 ? 6 : kTT == 2 ? 4 : 2;
-    return kTT <= 1 ? (kCT == 1 ? 8 : 6) : kTT == 2 ? 4 : 3; // 8 kCT + 4, 8, 16, 32
+    if (FewForm<kForm>::kQ4) // 4 kCT + 4, 16, 32, 64
+        return kCT <= 2 && kTT == 0 ? 8 : kTT <= 1 ? 4 : kTT == 4 && kCT == 4 ? 1 : 2;
+    return kTT <= 1 ? (kCT == 1 ? 8 : 4) : kTT == 2 ? 4 : 2; // 8 kCT + 4, 8, 16, 32
 }
 
-// Where the activation of `rows` rows from slot `base` on is: sixteen columns of all (padded) rows side by side.
+// The activation of the expert at place `at`.
 template <int kForm>
-__device__ __forceinline__ FewActs few_activation(const FewArgs &l, int base, int rows)
+__device__ __forceinline__ FewActs few_activation(const FewKernelArgs &g, const FewLists &lists, int at, int rows)
 {
-    constexpr int kElt = FewForm<kForm>::kElt;
-    const int padded = (rows + kRowPad<kForm> - 1) / kRowPad<kForm> * kRowPad<kForm>, cols = (l.F + 15) / 16 * 16;
-    return {static_cast<const unsigned char *>(l.a) + (int64_t)base * cols * kElt, (uint32_t)padded * (uint32_t)cols * kElt,
-            (uint32_t)padded * 16 * kElt, rows};
+    const uint32_t lines = __builtin_amdgcn_readfirstlane(lists.lines[at]), tiles = (uint32_t)g.f_tiles;
+    const uint32_t tile = few_tile_lines<kForm>(rows, g.width) * 128u;
+    return {static_cast<const unsigned char *>(g.l.a) + (int64_t)lines * tiles * 128, tiles * tile, g.width, tile, rows};
 }
 
-// Gate/up items of one class: (expert, 16 columns of F), every `step`-th; the eight wavefronts share the reduction.
+// Gate/up items of one class: (expert, `width` columns of F).  `split` wavefronts share an item's reduction, the workgroup
+// takes 8 / split items at a time, a round; a share's rounds are `shares` apart.
 template <int kForm, int kTT>
 struct GateUp {
     using Form = FewForm<kForm>;
+    static constexpr int kGate = kGateTiles<kForm>, kCT = 2 * kGate, kDepth = few_depth<kForm, kTT, kCT>();
+    static constexpr int kValues = kFewValues<kForm, kTT>;
+    const FewKernelArgs &g;
     const FewArgs &l;
     const FewLists &lists;
-    float *red; // [2][wavefront][gate, up][value][lane]
-    int count, share, lines, tiles;
-    int step_at, step_tile;
-    struct Place {
-        int at, tile;
-    } opening, closing_at;
+    float *red; // [rounds held][wavefront][tile][value][lane]
+    int begin, items, first, rounds, lines, part_lines, tiles;
 
-    __device__ GateUp(const FewArgs &l, const FewLists &lists, float *red, int cls, int who, int shares) : l(l), lists(lists), red(red)
+    // before: rounds of the classes before this one (rounds are numbered through all classes); it is moved on
+    __device__ GateUp(const FewKernelArgs &g, const FewLists &lists, float *red, int cls, int who, int &before)
+        : g(g), l(g.l), lists(lists), red(red), lines(g.h_lines), part_lines(g.part_lines), tiles(g.f_tiles)
     {
-        tiles = (l.F + 15) / 16;
-        lines = (l.H + Form::kLineCols - 1) / Form::kLineCols;
-        share = (lines + kFewWaves - 1) / kFewWaves;
-        const int begin = __builtin_amdgcn_readfirstlane(lists.begin[cls]), end = __builtin_amdgcn_readfirstlane(lists.begin[cls + 1]);
-        // items are numbered through all classes; those of a share are `shares` apart
-        const int skip = (int)((unsigned)begin * (unsigned)tiles % (unsigned)shares), first = who >= skip ? who - skip : who - skip + shares;
-        const int items = (end - begin) * tiles;
-        count = first < items ? (items - 1 - first) / shares + 1 : 0;
-        opening = closing_at = {begin + first / tiles, first % tiles};
-        step_at = shares / tiles;
-        step_tile = shares % tiles;
+        begin = __builtin_amdgcn_readfirstlane(lists.begin[cls]);
+        items = (__builtin_amdgcn_readfirstlane(lists.begin[cls + 1]) - begin) * tiles;
+        const int all = (items + kFewWaves / g.split - 1) / (kFewWaves / g.split);
+        first = who - (before ? before % g.shares : 0);
+        if (first < 0)
+            first += g.shares;
+        rounds = first < all ? (all - 1 - first) / g.shares + 1 : 0;
+        before += all;
     }
-    __device__ __forceinline__ void advance(Place &p) const
-    {
-        p.at += step_at;
-        p.tile += step_tile;
-        if (p.tile >= tiles)
-            p.tile -= tiles, ++p.at;
-    }
-    __device__ __forceinline__ int segments() const { return count; }
-    __device__ __forceinline__ int length(int) const { return share; }
+    __device__ __forceinline__ int wave() const { return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); }
+    __device__ __forceinline__ int item_of(int round, int sub) const { return (first + round * g.shares) * (kFewWaves / g.split) + sub; }
+    __device__ __forceinline__ int segments() const { return rounds; }
+    __device__ __forceinline__ int groups(int) const { return (part_lines + kDepth - 1) / kDepth; }
     __device__ __forceinline__ bool ready() const { return true; }
-    __device__ __forceinline__ void open(FewCursor<kForm, kTT, 2> &c, int)
+    __device__ __forceinline__ void open(FewCursor<kForm, kTT, kCT, false> &c, int round)
     {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-        const int expert = __builtin_amdgcn_readfirstlane(lists.expert[opening.at]), base = __builtin_amdgcn_readfirstlane(lists.base[opening.at]);
-        const int rows = __builtin_amdgcn_readfirstlane(lists.rows[opening.at]);
-        const int64_t row = (int64_t)expert * l.F + opening.tile * 16, end = (int64_t)(expert + 1) * l.F;
-        c.panel[0] = panel_of<kForm>(l.gate, row, end, l.H, l.scale_cols_h);
-        c.panel[1] = panel_of<kForm>(l.up, row, end, l.H, l.scale_cols_h);
-        const uint32_t x_row = (uint32_t)l.H * Form::kElt;
-        c.set_acts({static_cast<const unsigned char *>(l.x), (uint32_t)l.N * x_row, 16 * Form::kElt, rows},
-                   [&](int r) { return lists.token[base + r] * x_row; });
-        c.line = wave * share;
-        c.left = share;
-        c.lines = lines;
-        advance(opening);
-    }
-    __device__ __forceinline__ void close(const FewSums<kForm, kTT, 2> &sums, int k)
-    {
-        constexpr int kValues = kFewValues<kForm, kTT>;
-        const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-        float *const mine = red + (k % 2) * (kFewWaves * 2 * kValues * kWave);
+        const int item = item_of(round, wave() / g.split), part = wave() % g.split;
+        const bool there = item < items;
+        const int at = begin + (there ? item / tiles : 0), f0 = there ? item % tiles * g.width : 0;
+        const int expert = __builtin_amdgcn_readfirstlane(lists.expert[at]), base = __builtin_amdgcn_readfirstlane(lists.base[at]);
+        const int rows = __builtin_amdgcn_readfirstlane(lists.rows[at]);
+        const int64_t row = (int64_t)expert * l.F + f0, end = row + (l.F - f0 < g.width ? l.F - f0 : g.width);
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
+        for (int p = 0; p < kGate; ++p) {
+            c.panel[p] = panel_of<kForm>(l.gate, row + 16 * p, end, l.H, l.scale_cols_h);
+            c.panel[kGate + p] = panel_of<kForm>(l.up, row + 16 * p, end, l.H, l.scale_cols_h);
+        }
+        const uint32_t x_row = (uint32_t)l.H * Form::kElt;
+        c.set_acts({static_cast<const unsigned char *>(l.x), (uint32_t)l.N * x_row, 0, 0, rows},
+                   [&](int r) { return lists.token[base + r] * x_row; });
+        c.line = part * part_lines;
+        c.end = !there ? 0 : c.line + part_lines < lines ? c.line + part_lines : lines;
+        c.groups = groups(round);
+    }
+    __device__ __forceinline__ void close(const FewSums<kForm, kTT, kCT> &sums, int round)
+    {
+        const int lane = threadIdx.x % kWave;
+        float *const mine = red + round % kRoundsHeld<kForm, kTT> * kRoundFloats<kForm, kTT>;
+        if (kRoundsHeld<kForm, kTT> == 1)
+            few_barrier(); // the round before is read
+#pragma unroll
+        for (int c = 0; c < kCT; ++c)
 #pragma unroll
             for (int v = 0; v < kValues; ++v)
-                mine[((wave * 2 + c) * kValues + v) * kWave + lane] = sums.value(c, v);
-        few_barrier(); // (the other half's readers were done before its writers came here)
-        const int at = closing_at.at, f0 = closing_at.tile * 16;
-        advance(closing_at);
-        for (int v = (wave + k) % kFewWaves; v < kValues; v += kFewWaves) {
-            float total[2];
+                mine[((wave() * kCT + c) * kValues + v) * kWave + lane] = sums.value(c, v);
+        few_barrier(); // (with room for two: the readers of the round before last were done before anyone came here)
+        // unit: sixteen columns of an item and a value of the lanes
+        const int units = kFewWaves / g.split * kGate * kValues;
+        for (int unit = (wave() + round) % kFewWaves; unit < units; unit += kFewWaves) {
+            const int sub = unit / (kGate * kValues), p = unit / kValues % kGate, v = unit % kValues, item = item_of(round, sub);
+            if (item >= items)
+                continue;
+            const float *from = mine + ((sub * g.split * kCT + p) * kValues + v) * kWave + lane;
+            float part[2][kFewWaves];
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                total[c] = mine[(c * kValues + v) * kWave + lane];
+            for (int w = 0; w < kFewWaves; ++w) // (past the split: read for nothing, inside the round's sums all the same)
 #pragma unroll
-                for (int w = 1; w < kFewWaves; ++w)
-                    total[c] += mine[((w * 2 + c) * kValues + v) * kWave + lane];
+                for (int u = 0; u < 2; ++u)
+                    part[u][w] = from[((w < g.split ? w : 0) * kCT + u * kGate) * kValues * kWave];
+            float gate = part[0][0], up = part[1][0];
+#pragma unroll
+            for (int w = 1; w < kFewWaves; ++w) {
+                gate += w < g.split ? part[0][w] : 0.0f;
+                up += w < g.split ? part[1][w] : 0.0f;
             }
-            const float a = silu_mul_f32(total[0], total[1]);
-            const int base = __builtin_amdgcn_readfirstlane(lists.base[at]), rows = __builtin_amdgcn_readfirstlane(lists.rows[at]);
-            const FewActs to = few_activation<kForm>(l, base, rows);
-            const int r = few_row_of<kForm, kTT>(v), i = lane % 16;
-            const bool there = r < rows && f0 + i < l.F;
-            unsigned char *const tile = const_cast<unsigned char *>(to.data) + (int64_t)(f0 / 16) * to.tile + (r * 16 + i) * Form::kElt;
+            const float a = silu_mul_f32(gate, up);
+            const int at = begin + item / tiles, tile = item % tiles;
+            const int rows = __builtin_amdgcn_readfirstlane(lists.rows[at]);
+            const FewActs to = few_activation<kForm>(g, lists, at, rows);
+            const int r = few_row_of<kForm, kTT>(v), i = 16 * p + lane % 16;
+            const bool there = r < rows && i < g.width && tile * g.width + i < l.F;
+            unsigned char *const put = const_cast<unsigned char *>(to.data) + (int64_t)tile * to.tile + (r * g.width + i) * Form::kElt;
             if constexpr (kForm == kFewF32) {
                 if (there)
-                    __hip_atomic_store(reinterpret_cast<uint32_t *>(tile), __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            } else { // the even lane stores both columns (F is even)
+                    __hip_atomic_store(reinterpret_cast<uint32_t *>(put), __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            } else { // the even lane stores both columns (F and width are even)
                 const uint32_t both = pack_bf16x2(a, __shfl_xor(a, 1));
                 if (there && lane % 2 == 0)
-                    __hip_atomic_store(reinterpret_cast<uint32_t *>(tile), both, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    __hip_atomic_store(reinterpret_cast<uint32_t *>(put), both, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
         }
     }
@@ -317,48 +350,48 @@ struct GateUp {
 template <int kForm, int kTT, int kCT, class Ready>
 struct Down {
     using Form = FewForm<kForm>;
+    static constexpr int kDepth = few_depth<kForm, kTT, kCT>();
+    const FewKernelArgs &g;
     const FewArgs &l;
     const FewLists &lists;
     float *token_sums;
     int h0, cols;
     Ready wait;
-    int lines, begin, from, to;
+    int lines, begin, from, to, first;
 
-    __device__ Down(const FewArgs &l, const FewLists &lists, float *token_sums, int cls, int h0, int cols, Ready wait)
-        : l(l), lists(lists), token_sums(token_sums), h0(h0), cols(cols), wait(wait)
+    __device__ Down(const FewKernelArgs &g, const FewLists &lists, float *token_sums, int cls, int h0, int cols, Ready wait)
+        : g(g), l(g.l), lists(lists), token_sums(token_sums), h0(h0), cols(cols), wait(wait)
     {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-        lines = (l.F + Form::kLineCols - 1) / Form::kLineCols;
+        lines = g.f_lines;
         begin = __builtin_amdgcn_readfirstlane(lists.begin[cls]);
         const int64_t all = (int64_t)(__builtin_amdgcn_readfirstlane(lists.begin[cls + 1]) - begin) * lines;
         from = (int)(all * wave / kFewWaves);
         to = (int)(all * (wave + 1) / kFewWaves);
+        first = from / lines;
     }
-    __device__ __forceinline__ int segments() const { return to > from ? (to - 1) / lines - from / lines + 1 : 0; }
-    __device__ __forceinline__ int first_line(int k) const { return k ? 0 : from % lines; }
-    __device__ __forceinline__ int length(int k) const
-    {
-        const int start = k ? (from / lines + k) * lines : from, end = (from / lines + k + 1) * lines;
-        return (end < to ? end : to) - start;
-    }
+    __device__ __forceinline__ int segments() const { return to > from ? (to - 1) / lines - first + 1 : 0; }
+    __device__ __forceinline__ int start_of(int k) const { return k ? (first + k) * lines : from; }
+    __device__ __forceinline__ int end_of(int k) const { return (first + k + 1) * lines < to ? (first + k + 1) * lines : to; }
+    __device__ __forceinline__ int groups(int k) const { return (end_of(k) - start_of(k) + kDepth - 1) / kDepth; }
     __device__ __forceinline__ bool ready() { return wait(); }
-    __device__ __forceinline__ void open(FewCursor<kForm, kTT, kCT> &c, int k)
+    __device__ __forceinline__ void open(FewCursor<kForm, kTT, kCT, true> &c, int k)
     {
-        const int at = begin + from / lines + k;
-        const int expert = __builtin_amdgcn_readfirstlane(lists.expert[at]), base = __builtin_amdgcn_readfirstlane(lists.base[at]);
-        const int rows = __builtin_amdgcn_readfirstlane(lists.rows[at]);
+        const int at = begin + first + k;
+        const int expert = __builtin_amdgcn_readfirstlane(lists.expert[at]), rows = __builtin_amdgcn_readfirstlane(lists.rows[at]);
         const int64_t row = (int64_t)expert * l.H + h0, end = row + cols;
 #pragma unroll
         for (int p = 0; p < kCT; ++p)
             c.panel[p] = panel_of<kForm>(l.down, row + 16 * p, end, l.F, l.scale_cols_f);
-        c.set_acts(few_activation<kForm>(l, base, rows), [&](int r) { return (uint32_t)(r * 16 * Form::kElt); });
-        c.line = first_line(k);
-        c.left = length(k);
-        c.lines = lines;
+        const uint32_t a_row = (uint32_t)g.width * Form::kElt;
+        c.set_acts(few_activation<kForm>(g, lists, at, rows), [&](int r) { return r * a_row; });
+        c.line = start_of(k) - (first + k) * lines;
+        c.end = end_of(k) - (first + k) * lines;
+        c.groups = groups(k);
     }
     __device__ __forceinline__ void close(const FewSums<kForm, kTT, kCT> &sums, int k)
     {
-        const int at = begin + from / lines + k;
+        const int at = begin + first + k;
         const int base = __builtin_amdgcn_readfirstlane(lists.base[at]), rows = __builtin_amdgcn_readfirstlane(lists.rows[at]);
 #pragma unroll
         for (int v = 0; v < kFewValues<kForm, kTT>; ++v) {
@@ -380,7 +413,7 @@ template <int kForm, int kMaxTT, int kCT>
 __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int kRed = 2 * kFewWaves * 2 * (kMaxTT > 1 ? 4 * kMaxTT : 4) * kWave, kSums = kFewWaves * 16 * kMaxTT * 16 * kCT;
+    constexpr int kRed = kRoundFloats<kForm, kMaxTT> * kRoundsHeld<kForm, kMaxTT>, kSums = kFewWaves * 16 * kMaxTT * 16 * kCT;
     __shared__ union {
         FewRouting routing;
         float red[kRed];
@@ -428,16 +461,20 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
         }
     }
     __syncthreads();
-    few_make_lists<kForm>(lists, sh.routing, l.N, l.K, l.E);
+    few_make_lists<kForm>(lists, sh.routing, l.N, l.K, l.E, g.width);
 
     uint32_t *const share_flags = g.flags + 32;
     const FewCols in = {l.H, l.scale_cols_h, l.group}, mid = {l.F, l.scale_cols_f, l.group};
     bool all_there = false;
     for (int who = blockIdx.x;;) {
+        int before = 0;
         auto gate_up = [&](auto tt, int cls) {
             constexpr int kTT = decltype(tt)::value;
-            GateUp<kForm, kTT> items(l, lists, sh.red, cls, who, g.shares);
-            few_stream<kForm, kTT, 2, few_depth<kForm, kTT, 2>()>(items, in);
+            if (__builtin_amdgcn_readfirstlane(lists.begin[cls]) == __builtin_amdgcn_readfirstlane(lists.begin[cls + 1]))
+                return;
+            using Items = GateUp<kForm, kTT>;
+            Items items(g, lists, sh.red, cls, who, before);
+            few_stream<kForm, kTT, Items::kCT, Items::kDepth, false>(items, in);
             few_barrier(); // (the next one writes red)
         };
         gate_up(std::integral_constant<int, 0>{}, 0);
@@ -466,8 +503,9 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
                 constexpr int kTT = decltype(tt)::value;
                 if (missing >= 0 || __builtin_amdgcn_readfirstlane(lists.begin[cls]) == __builtin_amdgcn_readfirstlane(lists.begin[cls + 1]))
                     return;
-                Down<kForm, kTT, kCT, decltype(wait)> part(l, lists, mine, cls, h0, cols, wait);
-                few_stream<kForm, kTT, kCT, few_depth<kForm, kTT, kCT>()>(part, mid);
+                using Part = Down<kForm, kTT, kCT, decltype(wait)>;
+                Part part(g, lists, mine, cls, h0, cols, wait);
+                few_stream<kForm, kTT, kCT, Part::kDepth, true>(part, mid);
             };
             down(std::integral_constant<int, 0>{}, 0);
             down(std::integral_constant<int, 1>{}, 1);

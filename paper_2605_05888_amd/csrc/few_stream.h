@@ -11,12 +11,13 @@
 // each; chunk t of lane q are the columns
 //   bf16   32 t +  8 q ..   two 16-byte loads per line, four lanes side by side read 64 bytes
 //   fp32   16 t +  4 q ..   (four instructions of four columns each per chunk)
-//   FP4    32 q +  8 t ..   one 16-byte load: a lane has a whole group of 32 columns, so it needs one scale byte, which the
-//                           conversion to bf16 multiplies in (a power of two: exact)
-//   INT4   32 t +  8 q ..   one 16-byte load of columns 32 q .., then a transposition between the four lanes: an instruction
-//                           then covers one group of 32 columns, and the scale is applied to its sum in fp32.  A code c is
-//                           the bf16 number 128 + c (a byte beside 0x43); 136 times the sum of the activations, which an
-//                           instruction with ones gives, is subtracted.  (A weight times its scale would have to be rounded.)
+//   4 bits 32 t +  8 q ..   one 16-byte load of columns 32 q .., then a transposition between the four lanes: an instruction
+//                           then covers one group of 32 columns, and four lanes side by side read 64 bytes of activations
+// FP4 codes become bf16 numbers times their scale on the way (a power of two: exact).  INT4: the scale is applied to an
+// instruction's sum in fp32 (a weight times its scale would have to be rounded).  A code c is the bf16 number 128 + c (a byte
+// beside 0x43); 136 times the sum of the activations, which an instruction with ones gives, is subtracted.
+// Scales are loaded for four lines at once, lane q those of line q: a load costs the address unit the same sixteen rows
+// whether it fetches a byte a row or sixteen (a byte per lane and line: the unit was busy 0.73 of the time).
 //
 // kTT > 0: up to 16 kTT rows.  Row 16 tt + i of the activations is in lane i, kChunks loads per line and 16 rows.
 // kTT = 0: at most 16 / kChunks rows (kFewRows), one load per line: lane i holds chunk i % kChunks of row i / kChunks.  The
@@ -47,7 +48,7 @@ struct FewForm {
     __host__ __device__ static constexpr int64_t row_bytes(int64_t cols) { return kQ4 ? cols / 2 : cols * kElt; }
 };
 
-constexpr uint32_t kNowhere = 0x80000000u; // an offset past every byte count used here: loads give zeros
+constexpr uint32_t kNowhere = 0x40000000u; // an offset past every byte count used here, twice too: loads give zeros
 
 #if defined(__HIP_DEVICE_COMPILE__)
 
@@ -76,12 +77,13 @@ __device__ __forceinline__ Panel panel_of(const FewMatrix &w, int64_t row, int64
     return p;
 }
 
-// Where the activations of a segment are: row r, column c at row_of(r) + c / 16 * tile + c % 16 elements, all below `bytes`.
-// (Row-major matrices: tile is sixteen elements.)
+// Where the activations of a segment are.  Row-major (width 0): rows at row_of(r).  Else tiles of `width` columns (8, 16, 24 or 32), `tile` bytes apart, and in a tile the rows
+// at row_of(r).  All below `bytes`.
 struct FewActs {
     const unsigned char *data;
     uint32_t bytes;
-    uint32_t tile; // bytes
+    int width;
+    uint32_t tile;
     int rows;
 };
 
@@ -104,7 +106,6 @@ template <int kForm, int kTT, int kCT>
 struct FewOperands {
     static constexpr int kRows = kTT ? kTT : 1, kActs = kTT ? FewForm<kForm>::kChunks : 1;
     u32x4 w[kCT][FewForm<kForm>::kLoads];
-    uint32_t scale[kCT];
     u32x4 a[kRows][kActs];
 };
 
@@ -181,8 +182,47 @@ __device__ __forceinline__ u32x4 transpose_quads(u32x4 w)
     return u32x4{c[0], d[0], c[1], d[1]};
 }
 
+// Scales of four lines: as loaded (lane q: those of line q, FP4 four bytes, INT4 up to four bf16), and for every lane.
+template <int kForm, int kCT>
+struct FewScales {
+    static constexpr int kRegs = kForm == kFewInt4 ? 2 : 1;
+    uint32_t raw[kCT][kRegs];
+    uint32_t shift[kCT]; // bits that a load was moved back by, so as not to pass the panel's end
+    uint32_t of[kCT][4][kRegs];
+
+    __device__ __forceinline__ void spread()
+    {
+#pragma unroll
+        for (int c = 0; c < kCT; ++c) {
+            if constexpr (kForm == kFewInt4) {
+                const uint64_t v = ((uint64_t)raw[c][1] << 32 | raw[c][0]) >> (shift[c] & 63);
+                raw[c][0] = (uint32_t)v, raw[c][1] = (uint32_t)(v >> 32);
+            } else {
+                raw[c][0] >>= shift[c];
+            }
+#pragma unroll
+            for (int r = 0; r < kRegs; ++r) {
+                const auto pair = __builtin_amdgcn_permlane16_swap(raw[c][r], raw[c][r], false, false);
+                const auto even = __builtin_amdgcn_permlane32_swap(pair[0], pair[0], false, false);
+                const auto odd = __builtin_amdgcn_permlane32_swap(pair[1], pair[1], false, false);
+                of[c][0][r] = even[0], of[c][2][r] = even[1];
+                of[c][1][r] = odd[0], of[c][3][r] = odd[1];
+            }
+        }
+    }
+    // of group t of 32 columns in line d (0 .. 3)
+    __device__ __forceinline__ float fp4(int c, int d, int t) const { return fp4_scale(of[c][d][0] >> (8 * t) & 0xFFu); }
+    __device__ __forceinline__ float int4(int c, int d, int place) const
+    {
+        const uint32_t v = of[c][d][kRegs == 2 ? place / 2 : 0];
+        return __uint_as_float(place % 2 ? v & 0xFFFF0000u : v << 16);
+    }
+};
+
+// Line d of four.
 template <int kForm, int kTT, int kCT>
-__device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, const FewOperands<kForm, kTT, kCT> &o, int group)
+__device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, const FewOperands<kForm, kTT, kCT> &o,
+                                             const FewScales<kForm, kCT> &scales, int d, int group)
 {
     using Form = FewForm<kForm>;
     using Ops = FewOperands<kForm, kTT, kCT>;
@@ -203,12 +243,14 @@ __device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, con
     } else if constexpr (kForm != kFewInt4) {
 #pragma unroll
         for (int c = 0; c < kCT; ++c) {
-            const float scale = kForm == kFewFp4 ? fp4_scale(o.scale[c]) : 0.0f;
+            u32x4 codes;
+            if constexpr (kForm == kFewFp4)
+                codes = transpose_quads(o.w[c][0]);
 #pragma unroll
             for (int t = 0; t < Form::kChunks; ++t) {
                 bf16x8 w;
                 if constexpr (kForm == kFewFp4)
-                    w = fp4_operand(o.w[c][0][t], scale);
+                    w = fp4_operand(codes[t], scales.fp4(c, d, t));
                 else
                     w = __builtin_bit_cast(bf16x8, o.w[c][t]);
 #pragma unroll
@@ -220,30 +262,36 @@ __device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, con
         }
     } else {
         const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
-        // the scales of the line's four groups of 32 columns, for every lane q
-        float scale[kCT][4];
-        u32x4 w[kCT];
-#pragma unroll
-        for (int c = 0; c < kCT; ++c) {
-            const uint32_t s = o.scale[c] << 16;
-            const auto pair = __builtin_amdgcn_permlane16_swap(s, s, false, false);
-            const auto even = __builtin_amdgcn_permlane32_swap(pair[0], pair[0], false, false);
-            const auto odd = __builtin_amdgcn_permlane32_swap(pair[1], pair[1], false, false);
-            scale[c][0] = __uint_as_float(even[0]), scale[c][2] = __uint_as_float(even[1]);
-            scale[c][1] = __uint_as_float(odd[0]), scale[c][3] = __uint_as_float(odd[1]);
-            w[c] = transpose_quads(o.w[c][0]);
-        }
         if constexpr (kTT == 0) {
             const bf16x8 a = int4_order(o.a[0][0]);
             const f32x4 sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, ones, zero, 0, 0, 0);
+            const int shift = group == 32 ? 0 : group == 64 ? 1 : 2;
 #pragma unroll
-            for (int c = 0; c < kCT; ++c)
+            for (int c = 0; c < kCT; ++c) {
+                const u32x4 codes = transpose_quads(o.w[c][0]);
+                float v[4];
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
-                    const f32x4 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, int4_operand(w[c][t]), zero, 0, 0, 0);
-                    sums.one[c] = fmaf(scale[c][t], fmaf(-136.0f, sum[t], d[t]), sums.one[c]);
+                    const f32x4 p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, int4_operand(codes[t]), zero, 0, 0, 0);
+                    v[t] = fmaf(-136.0f, sum[t], p[t]);
                 }
+                if (shift == 0) {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        sums.one[c] = fmaf(scales.int4(c, d, t), v[t], sums.one[c]);
+                } else if (shift == 1) {
+                    sums.one[c] = fmaf(scales.int4(c, d, 0), v[0] + v[1], sums.one[c]);
+                    sums.one[c] = fmaf(scales.int4(c, d, 1), v[2] + v[3], sums.one[c]);
+                } else {
+                    sums.one[c] = fmaf(scales.int4(c, d, 0), (v[0] + v[1]) + (v[2] + v[3]), sums.one[c]);
+                }
+                __builtin_amdgcn_sched_barrier(0); // (else the products of all tiles are alive at once)
+            }
         } else {
+            u32x4 codes[kCT];
+#pragma unroll
+            for (int c = 0; c < kCT; ++c)
+                codes[c] = transpose_quads(o.w[c][0]);
             auto chained = [&](auto groups) { // of 32 columns under one scale
                 constexpr int kSame = decltype(groups)::value;
 #pragma unroll
@@ -259,14 +307,16 @@ __device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, con
                         }
 #pragma unroll
                         for (int c = 0; c < kCT; ++c) {
-                            f32x4 d = zero;
+                            f32x4 p = zero;
 #pragma unroll
                             for (int u = 0; u < kSame; ++u)
-                                d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[u], int4_operand(w[c][t + u]), d, 0, 0, 0);
+                                p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[u], int4_operand(codes[c][t + u]), p, 0, 0, 0);
+                            const float scale = scales.int4(c, d, t / kSame);
 #pragma unroll
                             for (int r = 0; r < 4; ++r)
-                                sums.acc[m][c][0][r] = fmaf(scale[c][t], fmaf(-136.0f, sum[r], d[r]), sums.acc[m][c][0][r]);
+                                sums.acc[m][c][0][r] = fmaf(scale, fmaf(-136.0f, sum[r], p[r]), sums.acc[m][c][0][r]);
                         }
+                        __builtin_amdgcn_sched_barrier(0);
                     }
             };
             if (group == 32)
@@ -279,22 +329,21 @@ __device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, con
     }
 }
 
-// The part of the stream that the next line is fetched from: panels and activations of one segment, for this lane.
-template <int kForm, int kTT, int kCT>
+// Where the stream's next lines are fetched from: panels and activations of one segment, for this lane.
+template <int kForm, int kTT, int kCT, bool kTiled>
 struct FewCursor {
     using Form = FewForm<kForm>;
     static constexpr int kRows = kTT ? kTT : 1, kActs = kTT ? Form::kChunks : 1;
     Panel panel[kCT];
     const unsigned char *act;
-    uint32_t act_bytes, act_line; // act_line: bytes from one line's activations to the next one's
-    uint32_t row_off[kRows], chunk_off[kActs];
-    int line, left, lines; // next line, lines left of this wavefront's, lines of a row
+    uint32_t act_bytes, act_tile, act_eights, act_magic; // eights: of columns in a tile; magic: 2^31 / eights, rounded up
+    uint32_t row_off[kRows];
+    int line, end, groups; // next line, the segment's last, groups of kDepth lines left
 
     // first column of chunk t of this lane's line
     static __device__ __forceinline__ int chunk_col(int t)
     {
-        const int q = threadIdx.x % kWave / 16;
-        return kForm == kFewFp4 ? 32 * q + 8 * t : (Form::kLineCols / Form::kChunks) * t + (16 / Form::kElt) * q;
+        return (Form::kLineCols / Form::kChunks) * t + (16 / Form::kElt) * (int)(threadIdx.x % kWave / 16);
     }
     template <class RowOf>
     __device__ __forceinline__ void set_acts(const FewActs &a, RowOf row_of)
@@ -302,45 +351,52 @@ struct FewCursor {
         const int i = threadIdx.x % 16;
         act = a.data;
         act_bytes = a.bytes;
-        act_line = (uint32_t)(Form::kLineCols / 16) * a.tile;
+        if constexpr (kTiled) {
+            act_tile = a.tile;
+            act_eights = (uint32_t)a.width / 8u;
+            act_magic = act_eights == 3 ? 0x2AAAAAABu : act_eights == 4 ? 0x20000000u : 0x80000000u >> (act_eights - 1);
+        }
 #pragma unroll
         for (int m = 0; m < kRows; ++m) {
             const int r = kTT ? 16 * m + i : i / Form::kChunks;
             row_off[m] = r < a.rows ? row_of(r) : kNowhere;
         }
-#pragma unroll
-        for (int t = 0; t < kActs; ++t) {
-            const int col = chunk_col(kTT ? t : i % Form::kChunks);
-            chunk_off[t] = (uint32_t)(col / 16) * a.tile + (uint32_t)(col % 16 * Form::kElt);
-        }
+    }
+    // Byte offset of a column in its row.
+    __device__ __forceinline__ uint32_t col_off(int col) const
+    {
+        if constexpr (!kTiled)
+            return (uint32_t)(col * Form::kElt);
+        const uint32_t n = (uint32_t)col / 8u, tile_at = __umulhi(2u * n, act_magic); // n / eights (n < 2^18)
+        return tile_at * act_tile + (n - tile_at * act_eights) * (8u * Form::kElt) + (uint32_t)(col % 8 * Form::kElt);
     }
 };
 
 // A wavefront's stream: segment after segment (a panel of weight rows with the activation rows that meet it, some lines of
 // both), without a gap in the loads between them.  The source says what they are:
 //   segments()            how many
-//   length(k)             lines of segment k, at least 1 (lines past the row's end read as zeros)
-//   open(cursor, k)       sets the cursor to segment k; k ascending, kDepth lines ahead of
+//   groups(k)             of kDepth lines in segment k, at least 1 (lines past its end read as zeros)
+//   open(cursor, k)       sets the cursor to segment k; k ascending, a group ahead of
 //   close(sums, k)        takes the sums of segment k
-//   ready()               called once, when the first weights are under way and before the first activations are asked for;
-//                         false: there are none, the stream ends
-template <int kForm, int kTT, int kCT, int kDepth, class Source>
+//   ready()               called once before the first load; false: the stream ends
+// A group is written out straight, so that what is waited for is the same on every path: segments change between groups only.
+// (With a change possible at every line the code is kDepth times as long, 180 KB, and waits for nearly everything in flight.)
+template <int kForm, int kTT, int kCT, int kDepth, bool kTiled, class Source>
 __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
 {
     using Form = FewForm<kForm>;
     using Ops = FewOperands<kForm, kTT, kCT>;
-    using Cursor = FewCursor<kForm, kTT, kCT>;
+    using Cursor = FewCursor<kForm, kTT, kCT, kTiled>;
     const int segments = source.segments();
-    if (segments == 0) {
-        (void)source.ready();
+    if (!source.ready() || segments == 0)
         return;
-    }
     const int lane = threadIdx.x % kWave, i = lane % 16, q = lane / 16;
     const uint32_t w_off = (uint32_t)i * (uint32_t)Form::row_bytes(g.cols) + (uint32_t)q * 16u;
-    const int scale_off = i * g.scale_cols;
-    const int group_shift = kForm == kFewInt4 ? (g.group == 32 ? 0 : g.group == 64 ? 1 : 2) : 0;
-    auto fetch_weights = [&](Ops &o, const Cursor &c) {
-        const bool there = c.line < c.lines; // (else no bytes: zeros, and the number of loads in flight stays)
+    constexpr int kFours = Form::kQ4 ? (kDepth + 3) / 4 : 1; // scale loads per group of lines
+    FewScales<kForm, kCT> scales[kFours];
+    Cursor c;
+    auto fetch = [&](Ops &o) {
+        const bool there = c.line < c.end; // (else no bytes: zeros, and the number of loads in flight stays)
 #pragma unroll
         for (int p = 0; p < kCT; ++p) {
             const auto rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(c.panel[p].data), 0,
@@ -348,85 +404,80 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
 #pragma unroll
             for (int s = 0; s < Form::kLoads; ++s) // (weights are read once: non-temporal)
                 o.w[p][s] = __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(w_off + (uint32_t)(c.line * Form::kLineBytes + 64 * s)), 0, 2);
-            if constexpr (Form::kQ4) {
-                const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(c.panel[p].scales), 0,
-                                                                  there ? (int)c.panel[p].scale_bytes : 0, 0x00020000);
-                const int at = scale_off + ((c.line * 4 + q) >> group_shift);
-                if constexpr (kForm == kFewFp4)
-                    o.scale[p] = __builtin_amdgcn_raw_buffer_load_b8(rs, at, 0, 0);
-                else
-                    o.scale[p] = __builtin_amdgcn_raw_buffer_load_b16(rs, 2 * at, 0, 0);
-            }
         }
-    };
-    auto fetch_acts = [&](Ops &o, const Cursor &c) {
-        const bool there = c.line < c.lines;
         const auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(c.act), 0, there ? (int)c.act_bytes : 0, 0x00020000);
-        const uint32_t base = (uint32_t)c.line * c.act_line;
-        const int col0 = c.line * Form::kLineCols;
 #pragma unroll
         for (int t = 0; t < Ops::kActs; ++t) {
-            // columns past the row's end would be another row's
-            const bool in = !Form::kRagged || col0 + Cursor::chunk_col(kTT ? t : i % Form::kChunks) < g.cols;
+            const int col = c.line * Form::kLineCols + Cursor::chunk_col(kTT ? t : i % Form::kChunks);
+            const uint32_t at = !Form::kRagged || col < g.cols ? c.col_off(col) : kNowhere; // (past the row's end would be another row's)
 #pragma unroll
             for (int m = 0; m < Ops::kRows; ++m)
-                o.a[m][t] = __builtin_amdgcn_raw_buffer_load_b128(ra, (int)(in ? c.row_off[m] + c.chunk_off[t] + base : kNowhere), 0, 0);
+                o.a[m][t] = __builtin_amdgcn_raw_buffer_load_b128(ra, (int)(at + c.row_off[m]), 0, 0);
         }
-    };
-    Cursor c;
-    int opened = 0; // segments
-    auto open = [&]() {
-        if (opened < segments) {
-            source.open(c, opened);
-            ++opened;
-        } else {
-            c.lines = 0; // nothing more
-            c.left = 0x7FFFFFFF;
-        }
-    };
-    auto advance = [&]() {
         ++c.line;
-        if (--c.left == 0)
-            open();
         // one order of the loads everywhere: else the wait at the top of the loop is for all of them
         __builtin_amdgcn_sched_barrier(0);
     };
-    Ops o[kDepth];
-    {
-        // The weights of the first lines go out before ready(), their activations after it.
-        Cursor starts[kDepth];
-        open();
+    // the scales of a group of lines, asked for before its first line
+    auto fetch_scales = [&]() {
+        if constexpr (Form::kQ4) {
+            constexpr int kBytes = kForm == kFewFp4 ? 1 : 2, kLoad = 4 * kBytes;
+            const int per_line = kForm == kFewFp4 || g.group == 32 ? 4 : g.group == 64 ? 2 : 1;
 #pragma unroll
-        for (int d = 0; d < kDepth; ++d) {
-            starts[d] = c;
-            fetch_weights(o[d], c);
-            advance();
+            for (int f = 0; f < kFours; ++f)
+#pragma unroll
+                for (int p = 0; p < kCT; ++p) {
+                    const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(c.panel[p].scales), 0,
+                                                                      c.line < c.end ? (int)c.panel[p].scale_bytes : 0, 0x00020000);
+                    const uint32_t want = (uint32_t)(i * g.scale_cols + (c.line + 4 * f + q) * per_line) * kBytes;
+                    const uint32_t last = c.panel[p].scale_bytes - kLoad, at = want < last ? want : last;
+                    scales[f].shift[p] = want - at < kLoad ? 8 * (want - at) : 0; // (further: of a row or line that is not there)
+                    if constexpr (kForm == kFewFp4) {
+                        scales[f].raw[p][0] = __builtin_amdgcn_raw_buffer_load_b32(rs, (int)at, 0, 0);
+                    } else {
+                        const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(rs, (int)at, 0, 0);
+                        scales[f].raw[p][0] = v[0], scales[f].raw[p][1] = v[1];
+                    }
+                }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        if (!source.ready())
-            return;
+    };
+    Ops o[kDepth];
+    int opened = 1;
+    source.open(c, 0);
+    fetch_scales();
 #pragma unroll
-        for (int d = 0; d < kDepth; ++d)
-            fetch_acts(o[d], starts[d]);
-        __builtin_amdgcn_sched_barrier(0);
-    }
+    for (int d = 0; d < kDepth; ++d)
+        fetch(o[d]);
     FewSums<kForm, kTT, kCT> sums;
     sums.clear();
-    int closing = 0, left = source.length(0);
+    int closing = 0, left = source.groups(0);
     for (;;) {
+        if (--c.groups == 0) { // the next group is another segment's
+            if (opened < segments)
+                source.open(c, opened++);
+            else
+                c.end = 0; // nothing more
+        }
+        if constexpr (Form::kQ4) {
+#pragma unroll
+            for (int f = 0; f < kFours; ++f)
+                scales[f].spread();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        fetch_scales();
 #pragma unroll
         for (int d = 0; d < kDepth; ++d) {
-            few_multiply(sums, o[d], g.group);
+            few_multiply(sums, o[d], scales[Form::kQ4 ? d / 4 : 0], d % 4, g.group);
             __builtin_amdgcn_sched_barrier(0);
-            if (--left == 0) {
-                source.close(sums, closing);
-                if (++closing == segments)
-                    return;
-                sums.clear();
-                left = source.length(closing);
-            }
-            fetch_weights(o[d], c);
-            fetch_acts(o[d], c);
-            advance();
+            fetch(o[d]);
+        }
+        if (--left == 0) {
+            source.close(sums, closing);
+            if (++closing == segments)
+                return;
+            sums.clear();
+            left = source.groups(closing);
         }
     }
 }

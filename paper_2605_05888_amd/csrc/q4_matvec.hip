@@ -9,7 +9,7 @@ constexpr int kMvWaves = 8;
 
 #if defined(__HIP_DEVICE_COMPILE__)
 // Rows [m0, m0 + rows) of x, at most 16 kTT (kTT = 0: 4), with weight rows [n0, n0 + 16 kCT) of matrix e.
-template <int kForm, int kTT, int kCT>
+template <int kForm, int kTT, int kCT, int kDepth>
 struct MatvecTile {
     using Form = FewForm<kForm>;
     const MatvecArgs &g;
@@ -20,35 +20,36 @@ struct MatvecTile {
     int64_t n0;
 
     __device__ __forceinline__ int lines() const { return (g.cols + Form::kLineCols - 1) / Form::kLineCols; }
-    __device__ __forceinline__ int first() const { return lines() * (int)__builtin_amdgcn_readfirstlane(threadIdx.x / kWave) / kMvWaves; }
-    __device__ __forceinline__ int last() const { return lines() * ((int)__builtin_amdgcn_readfirstlane(threadIdx.x / kWave) + 1) / kMvWaves; }
+    __device__ __forceinline__ int wave() const { return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); }
+    __device__ __forceinline__ int first() const { return lines() * wave() / kMvWaves; }
+    __device__ __forceinline__ int last() const { return lines() * (wave() + 1) / kMvWaves; }
     __device__ __forceinline__ int segments() const { return 1; }
-    __device__ __forceinline__ int length(int) const { return last() > first() ? last() - first() : 1; }
+    __device__ __forceinline__ int groups(int) const { return last() > first() ? (last() - first() + kDepth - 1) / kDepth : 1; }
     __device__ __forceinline__ bool ready() const { return true; }
-    __device__ __forceinline__ void open(FewCursor<kForm, kTT, kCT> &c, int) const
+    __device__ __forceinline__ void open(FewCursor<kForm, kTT, kCT, false> &c, int) const
     {
         const int64_t row = (int64_t)e * g.rows + n0, end = (int64_t)(e + 1) * g.rows;
 #pragma unroll
         for (int p = 0; p < kCT; ++p)
             c.panel[p] = panel_of<kForm>(g.w, row + 16 * p, end, g.cols, g.scale_cols);
         const uint32_t x_row = (uint32_t)g.cols * Form::kElt;
-        c.set_acts({static_cast<const unsigned char *>(g.x) + m0 * x_row, (uint32_t)rows * x_row, 16 * Form::kElt, rows},
+        c.set_acts({static_cast<const unsigned char *>(g.x) + m0 * x_row, (uint32_t)rows * x_row, 0, 0, rows},
                    [&](int r) { return r * x_row; });
-        c.line = last() > first() ? first() : lines(); // (fewer lines than wavefronts: some have none)
-        c.left = length(0);
-        c.lines = lines();
+        c.line = first();
+        c.end = last();
+        c.groups = groups(0);
     }
     __device__ __forceinline__ void close(const FewSums<kForm, kTT, kCT> &sums, int) const
     {
         constexpr int kValues = kFewValues<kForm, kTT>;
-        const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+        const int lane = threadIdx.x % kWave;
 #pragma unroll
         for (int c = 0; c < kCT; ++c)
 #pragma unroll
             for (int v = 0; v < kValues; ++v)
-                red[((wave * kCT + c) * kValues + v) * kWave + lane] = sums.value(c, v);
+                red[((wave() * kCT + c) * kValues + v) * kWave + lane] = sums.value(c, v);
         few_barrier();
-        for (int o = wave; o < kCT * kValues; o += kMvWaves) {
+        for (int o = wave(); o < kCT * kValues; o += kMvWaves) {
             float v = red[o * kWave + lane];
 #pragma unroll
             for (int w = 1; w < kMvWaves; ++w)
@@ -76,16 +77,16 @@ __global__ __launch_bounds__(kMvWaves *kWave, kMaxTT == 1 ? 4 : 2) void q4_matve
         const int rows = (int)(m1 - m0 < 16 * kMaxTT ? m1 - m0 : 16 * kMaxTT);
         const FewCols cols = {g.cols, g.scale_cols, g.group};
         auto tile = [&](auto tt, auto depth) {
-            constexpr int kTT = decltype(tt)::value;
-            MatvecTile<kForm, kTT, kCT> t = {g, red, e, m0, rows, n0};
-            few_stream<kForm, kTT, kCT, decltype(depth)::value>(t, cols);
+            constexpr int kTT = decltype(tt)::value, kDepth = decltype(depth)::value;
+            MatvecTile<kForm, kTT, kCT, kDepth> t = {g, red, e, m0, rows, n0};
+            few_stream<kForm, kTT, kCT, kDepth, false>(t, cols);
         };
         if (rows <= FewForm<kForm>::kFewRows)
             tile(std::integral_constant<int, 0>{}, std::integral_constant<int, 4>{});
         else if (kMaxTT == 1 || rows <= 16)
-            tile(std::integral_constant<int, 1>{}, std::integral_constant<int, 3>{});
+            tile(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
         else if (rows <= 32)
-            tile(std::integral_constant<int, (kMaxTT < 2 ? 1 : 2)>{}, std::integral_constant<int, 3>{});
+            tile(std::integral_constant<int, (kMaxTT < 2 ? 1 : 2)>{}, std::integral_constant<int, 4>{});
         else
             tile(std::integral_constant<int, kMaxTT>{}, std::integral_constant<int, 2>{});
     }

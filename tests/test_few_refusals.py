@@ -36,7 +36,7 @@ def test_workspace_sizes():
     assert hub.workspace_bytes(hub.OP_LAYER_FEW, N=5, H=516, E=12, K=3, F=1028, dtype=hub.F32) >= 15 * 1028 * 4
     good = dict(N=4, H=64, E=8, K=2, F=64, dtype=hub.BF16)
     assert hub.workspace_bytes(hub.OP_LAYER_FEW, **good) > 0
-    for bad in (dict(N=-1), dict(N=65), dict(H=0), dict(F=0), dict(H=1 << 22), dict(E=0), dict(E=2048), dict(K=0), dict(K=33),
+    for bad in (dict(N=-1), dict(N=65), dict(H=0), dict(F=0), dict(H=1 << 21), dict(E=0), dict(E=2048), dict(K=0), dict(K=33),
                 dict(dtype=7)):
         assert hub.workspace_bytes(hub.OP_LAYER_FEW, **{**good, **bad}) == 0, bad
 
@@ -68,7 +68,7 @@ LAYER = [
     (dict(dtype=5), -2, "dtype"), (dict(N=-1), -1, "N"), (dict(N=65), -2, "MOE_FEW_TOKENS"), (dict(K=0), -1, "K"),
     (dict(K=9), -1, "K"), (dict(E=64, K=33), -2, "MOE_MAX_TOPK"), (dict(E=1025), -2, "MOE_MAX_EXPERTS"), (dict(E=0, K=0), -1, "E"),
     (dict(mode=2), -1, "score_mode"), (dict(H=0), -1, "H"), (dict(H=60), -1, "16"), (dict(H=96), -2, "multiples of 64"),
-    (dict(F=96), -2, "multiples of 64"), (dict(F=0), -1, "F"), (dict(H=1 << 22), -2, "2^22"), (dict(F=1 << 22), -2, "2^22"),
+    (dict(F=96), -2, "multiples of 64"), (dict(F=0), -1, "F"), (dict(H=1 << 21), -2, "2^21"), (dict(F=1 << 21), -2, "2^21"),
     (dict(x=None), -1, "NULL"), (dict(x=A + 8), -1, "aligned"), (dict(W_r=None), -1, "NULL"), (dict(bias=A + 4), -1, "aligned"),
     (dict(idx=None), -1, "NULL"), (dict(w=None), -1, "NULL"), (dict(out=None), -1, "NULL"), (dict(out=A + 2), -1, "aligned"),
     (dict(ws=None), -3, "workspace"), (dict(ws_bytes=100), -3, "workspace"), (dict(ws=A + 16), -1, "128-byte"),
@@ -94,7 +94,7 @@ def test_layer_few_q4_refuses(change, code, word):
 
 @pytest.mark.parametrize("change,code,word", [
     (dict(dtype=5), -2, "dtype"), (dict(dtype=hub.F32), -2, "BF16"), (dict(M=-1), -1, "M"), (dict(M=1 << 31), -1, "M"),
-    (dict(cols=0), -1, "cols"), (dict(cols=96), -2, "multiple of 64"), (dict(cols=1 << 22), -1, "cols"), (dict(rows=0), -1, "rows"),
+    (dict(cols=0), -1, "cols"), (dict(cols=96), -2, "multiple of 64"), (dict(cols=1 << 21), -1, "cols"), (dict(rows=0), -1, "rows"),
     (dict(rows=4), -1, "16"), (dict(rows=1 << 27), -1, "rows"), (dict(E=0), -1, "E_local"), (dict(E=65536), -1, "E_local"),
     (dict(seg=None), -1, "seg_offsets"), (dict(fmt=-1), -1, "format"), (dict(group=128), -2, "group"), (dict(x=None), -1, "NULL"),
     (dict(codes=None), -1, "NULL"), (dict(scales=A + 2), -1, "aligned"), (dict(y=None), -1, "NULL")])
