@@ -24,6 +24,11 @@
 // instruction of chunk t then gives sense only in result rows i with i % kChunks == t, and every chunk has a result of its own:
 // with four chunks, register t of result t in lane q is row q's.  (An expert of a decoded batch mostly has that few rows.
 // Four times fewer loads and registers for the activations of 4-bit weights, and for INT4 one multiplication per scale.)
+//
+// In that layout neighbouring lanes hold different rows, and the address unit takes a load of sixteen bytes a lane four
+// neighbouring lanes at a time: 64 bytes of one line in a cycle, or four lines in four (fetched like that, the unit was busy
+// 0.6 - 0.8 of the time).  So lane l fetches what lane (l % 4, l / 4) of the layout needs, four neighbours 64 bytes of a row,
+// and the registers change lanes on arrival (ds_bpermute).
 #pragma once
 
 #include "common.h"
@@ -192,6 +197,7 @@ struct FewScales {
 
     __device__ __forceinline__ void spread()
     {
+        const int row = (int)(threadIdx.x % 16) * 16; // byte address of the lane that fetched line 0's of row i
 #pragma unroll
         for (int c = 0; c < kCT; ++c) {
             if constexpr (kForm == kFewInt4) {
@@ -201,13 +207,10 @@ struct FewScales {
                 raw[c][0] >>= shift[c];
             }
 #pragma unroll
-            for (int r = 0; r < kRegs; ++r) {
-                const auto pair = __builtin_amdgcn_permlane16_swap(raw[c][r], raw[c][r], false, false);
-                const auto even = __builtin_amdgcn_permlane32_swap(pair[0], pair[0], false, false);
-                const auto odd = __builtin_amdgcn_permlane32_swap(pair[1], pair[1], false, false);
-                of[c][0][r] = even[0], of[c][2][r] = even[1];
-                of[c][1][r] = odd[0], of[c][3][r] = odd[1];
-            }
+            for (int r = 0; r < kRegs; ++r)
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+                    of[c][d][r] = (uint32_t)__builtin_amdgcn_ds_bpermute(row + 4 * d, (int)raw[c][r]);
         }
     }
     // of group t of 32 columns in line d (0 .. 3)
@@ -219,14 +222,33 @@ struct FewScales {
     }
 };
 
+// What a lane has fetched, to the lane whose operand it is.
+__device__ __forceinline__ void to_operand_lane(u32x4 &v)
+{
+    const int from = (int)(threadIdx.x % 16 * 4 + threadIdx.x % kWave / 16) * 4;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        v[j] = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)v[j]);
+}
+
 // Line d of four.
 template <int kForm, int kTT, int kCT>
-__device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, const FewOperands<kForm, kTT, kCT> &o,
+__device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, FewOperands<kForm, kTT, kCT> &o,
                                              const FewScales<kForm, kCT> &scales, int d, int group)
 {
     using Form = FewForm<kForm>;
     using Ops = FewOperands<kForm, kTT, kCT>;
     const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int c = 0; c < kCT; ++c)
+#pragma unroll
+        for (int l = 0; l < Form::kLoads; ++l)
+            to_operand_lane(o.w[c][l]);
+#pragma unroll
+    for (int m = 0; m < Ops::kRows; ++m)
+#pragma unroll
+        for (int t = 0; t < Ops::kActs; ++t)
+            to_operand_lane(o.a[m][t]);
     if constexpr (kForm == kFewF32) {
 #pragma unroll
         for (int t = 0; t < Form::kChunks; ++t)
@@ -340,15 +362,15 @@ struct FewCursor {
     uint32_t row_off[kRows];
     int line, end, groups; // next line, the segment's last, groups of kDepth lines left
 
-    // first column of chunk t of this lane's line
+    // first column of chunk t that this lane fetches
     static __device__ __forceinline__ int chunk_col(int t)
     {
-        return (Form::kLineCols / Form::kChunks) * t + (16 / Form::kElt) * (int)(threadIdx.x % kWave / 16);
+        return (Form::kLineCols / Form::kChunks) * t + (16 / Form::kElt) * (int)(threadIdx.x % 4);
     }
     template <class RowOf>
     __device__ __forceinline__ void set_acts(const FewActs &a, RowOf row_of)
     {
-        const int i = threadIdx.x % 16;
+        const int i = threadIdx.x % kWave / 4;
         act = a.data;
         act_bytes = a.bytes;
         if constexpr (kTiled) {
@@ -390,7 +412,7 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
     const int segments = source.segments();
     if (!source.ready() || segments == 0)
         return;
-    const int lane = threadIdx.x % kWave, i = lane % 16, q = lane / 16;
+    const int i = threadIdx.x % kWave / 4, q = threadIdx.x % 4; // whose operand this lane fetches
     const uint32_t w_off = (uint32_t)i * (uint32_t)Form::row_bytes(g.cols) + (uint32_t)q * 16u;
     constexpr int kFours = Form::kQ4 ? (kDepth + 3) / 4 : 1; // scale loads per group of lines
     FewScales<kForm, kCT> scales[kFours];
