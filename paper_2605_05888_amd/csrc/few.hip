@@ -113,20 +113,20 @@ size_t few_workspace_bytes(int64_t N, int64_t H, int E, int K, int64_t F, int dt
     return few_carve(nullptr, N, E, K, F, dtype).bytes;
 }
 
-// Width and split of the gate/up items: the least time of the longest share, in units of a line of one column.  Narrow items
-// make even shares of little work (one token, 4 experts of 1408 columns: 22 columns per workgroup, three items of 8 or two of
-// 16), wide ones use their loads and registers better; a wavefront's lines go in groups of four.
-static void choose_items(FewKernelArgs &g, int widest, int line_cols)
+// Width of the gate/up items and parts of their reduction: the least time of the longest share, in units of a line of one
+// column per wavefront.  Narrow items make even shares of little work (one token, 4 experts of 1408 columns: 22 columns per
+// workgroup, three items of 8 or two of 16), wide ones use their loads and registers better; parts do the same for the
+// wavefronts of a workgroup, at the price of an exchange and of groups that are not full.
+static void choose_items(FewKernelArgs &g, double experts, int widest)
 {
-    const double touched = g.l.E * (1.0 - pow(1.0 - (double)g.l.K / g.l.E, g.l.N)); // experts, if all are equally popular
-    const int64_t experts = touched < 1.0 ? 1 : (int64_t)(touched + 0.5), lines = ceil_div(g.l.H, line_cols);
     int64_t least = INT64_MAX;
     for (int width = widest; width >= 8; width -= 8)
-        for (int split = kFewWaves; split >= 1; split /= 2) {
-            const int64_t rounds = ceil_div(ceil_div(experts * ceil_div(g.l.F, width), kFewWaves / split), g.shares);
-            const int64_t time = rounds * (ceil_div(ceil_div(lines, split), 4) * 4 * (width + 4) + 8);
+        for (int parts = 1; parts <= kFewWaves && (parts == 1 || parts <= g.h_lines); parts *= 2) {
+            const int64_t items = ceil_div((int64_t)(experts * (double)ceil_div(g.l.F, width) + 0.5), g.shares);
+            const int64_t turns = ceil_div(items * parts, kFewWaves);
+            const int64_t time = turns * (ceil_div(ceil_div(g.h_lines, parts), 4) * 4 * (width + 4) + (parts > 1 ? 40 : 20));
             if (time < least)
-                least = time, g.width = width, g.split = split;
+                least = time, g.width = width, g.gate_parts = parts;
         }
 }
 
@@ -140,15 +140,23 @@ int launch_layer_few(const FewArgs &args, int dtype, int format, hipStream_t st)
     g.parts = w.parts;
     g.flags = w.flags;
     g.shares = cus < kMaxShares ? cus : kMaxShares;
-    // columns of a down tile: as many tiles as workgroups (or a multiple), none wider than 32
-    const int64_t rounds = ceil_div(args.H, 32 * (int64_t)g.shares);
-    g.down_cols = (int)(ceil_div(ceil_div(args.H, rounds * g.shares), 4) * 4);
     const int line_cols = format != kNoFormat ? 128 : dtype == MOE_BF16 ? 64 : 32;
-    choose_items(g, format == MOE_Q4_FP4 ? 16 * kGateTiles<kFewFp4> : 16, line_cols);
     g.h_lines = (int)ceil_div(args.H, line_cols);
-    g.part_lines = (int)ceil_div(g.h_lines, g.split);
-    g.f_tiles = (int)ceil_div(args.F, g.width);
     g.f_lines = (int)ceil_div(args.F, line_cols);
+    const int rows = args.N * args.K;
+    const double touched = args.E * (1.0 - pow(1.0 - (double)args.K / args.E, args.N)); // experts, if all are equally popular
+    const double experts = touched < 1.0 ? 1.0 : touched;
+    choose_items(g, experts, format == MOE_Q4_FP4 ? 16 * kGateTiles<kFewFp4> : 16);
+    g.f_tiles = (int)ceil_div(args.F, g.width);
+    // columns of a down tile: as many tiles as workgroups (or a multiple), none wider than 32, or 16 where the rows' sums would
+    // not fit in LDS
+    const int64_t widest = rows * 32 <= kPoolFloats ? 32 : 16, rounds = ceil_div(args.H, widest * g.shares);
+    g.down_cols = (int)(ceil_div(ceil_div(args.H, rounds * g.shares), 4) * 4);
+    // parts of an expert there: some eight units for each wavefront, none shorter than four lines
+    const int row_floats = g.down_cols <= 16 ? 16 : 32;
+    for (g.down_parts = 1; g.down_parts < 16 && experts * g.down_parts < 8 * kFewWaves && g.f_lines >= 8 * g.down_parts &&
+                           2 * g.down_parts * rows * row_floats <= kPoolFloats;)
+        g.down_parts *= 2;
     const char *const patience = getenv("MOE_FEW_PATIENCE"); // (tests: 0 makes every workgroup take over what is missing)
     g.patience = patience ? atoi(patience) : kDefaultPatience;
     const dim3 grid((unsigned)(ceil_div(args.E, 16) * kParts), (unsigned)ceil_div(args.N, 16));

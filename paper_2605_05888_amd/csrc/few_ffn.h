@@ -7,12 +7,14 @@
 // per compute unit, with a fixed share of each step:
 //   tokens   (more than kRouteAll) top-K of eight tokens, one per wavefront; up to kRouteAll tokens every workgroup selects
 //            for itself, which is quicker than waiting for another's answer
-//   gate/up  items (expert, 16 columns of F): both products of the expert's rows and the activation, into the workspace.
-//            The wavefronts share the reduction; a wavefront's stream of weights runs on from item to item
+//   gate/up  items (expert, a few columns of F): both products of the expert's rows and the activation, into the workspace
 //   down     a few columns of H over ALL touched experts (as many as make a share for every workgroup): a token's sum over
-//            its K experts is made in one workgroup, so there is no third exchange and equal calls give equal bits
-// Shares are fixed because drawing them costs more than it gives: atomics on one address are served one in 12 ns (512
-// workgroups that drew from one counter and polled another: one token 64 us instead of 20).
+//            its K experts is made in one workgroup, in ascending k, so there is no third exchange
+// Within a workgroup the wavefronts draw their work, items or parts of items, from counters in LDS: served unequally by the
+// memory, they would wait for each other a fifth of the time otherwise.  What is added up, and in which order, does not depend
+// on who draws what: partial sums meet in LDS and are added by their place, so equal calls give equal bits.
+// Shares of workgroups are fixed because drawing them costs more than it gives: atomics on one address in memory are served
+// one in 12 ns (512 workgroups that drew from one counter and polled another: one token 64 us instead of 27).
 //
 // What a step needs from other workgroups is said by a flag per share.  A workgroup that has waited for longer than any share
 // takes does the missing share itself (a second time, with the same bits, if its owner is only late): every wait ends, however
@@ -47,22 +49,19 @@ struct FewKernelArgs {
     const float *parts;
     uint32_t *flags;
     int shares;    // of gate/up items
-    int width;     // columns of F of an item: a multiple of 8, at most 16 * kGateTiles
-    int split;     // wavefronts that share an item's reduction: 8, 4, 2 or 1
-    int down_cols; // columns of H of a down tile, at most 16 kCT
+    int width;      // columns of F of an item: a multiple of 8, at most 16 * kGateTiles
+    int gate_parts; // of an item's reduction: 1, 2, 4 or 8
+    int down_cols;  // columns of H of a down tile, at most 16 kCT
+    int down_parts; // of an expert's reduction there
     int patience;
-    int h_lines, part_lines, f_tiles, f_lines; // lines of H, of a wavefront's part of them; items' tiles of F; lines of F
+    int h_lines, f_lines, f_tiles; // lines of H and F; items of an expert
 };
 
 // Sixteens of columns of a gate/up item, each of both matrices.
 template <int kForm>
 constexpr int kGateTiles = kForm == kFewFp4 ? 2 : 1;
 
-// A round's partial sums in LDS (all wavefronts), and how many rounds' there are room for.
-template <int kForm, int kTT>
-constexpr int kRoundFloats = kFewWaves * 2 * kGateTiles<kForm> * (kTT ? 4 * kTT : 4 / FewForm<kForm>::kChunks) * kWave;
-template <int kForm, int kTT>
-constexpr int kRoundsHeld = kRoundFloats<kForm, kTT> > 16384 ? 1 : 2;
+constexpr int kPoolFloats = 32768; // LDS for partial sums
 
 #if defined(__HIP_DEVICE_COMPILE__)
 __device__ __forceinline__ float silu_mul_f32(float g, float u) { return g / (1.0f + expf(-g)) * u; }
@@ -95,7 +94,8 @@ struct FewLists {
     uint16_t expert[MOE_MAX_EXPERTS], base[MOE_MAX_EXPERTS];
     uint16_t lines[MOE_MAX_EXPERTS]; // cache lines of one activation tile before this expert's
     uint8_t rows[MOE_MAX_EXPERTS];
-    uint8_t token[kMaxRows];
+    uint8_t token[kMaxRows]; // of a slot
+    uint16_t slot[kMaxRows]; // of n * K + k, and its weight
     float weight[kMaxRows];
 };
 struct FewRouting { // while the lists are made
@@ -184,7 +184,8 @@ __device__ __forceinline__ void few_make_lists(FewLists &lists, FewRouting &r, i
         const int e = r.pick[p], n = p / K;
         const int s = r.first[e] + (int)__popcll(r.mask[e] & ((1ull << n) - 1));
         lists.token[s] = (uint8_t)n;
-        lists.weight[s] = r.weight[p];
+        lists.slot[p] = (uint16_t)s;
+        lists.weight[p] = r.weight[p];
     }
     __syncthreads();
 }
@@ -244,42 +245,64 @@ __device__ __forceinline__ FewActs few_activation(const FewKernelArgs &g, const 
     return {static_cast<const unsigned char *>(g.l.a) + (int64_t)lines * tiles * 128, tiles * tile, g.width, tile, rows};
 }
 
-// Gate/up items of one class: (expert, `width` columns of F).  `split` wavefronts share an item's reduction, the workgroup
-// takes 8 / split items at a time, a round; a share's rounds are `shares` apart.
+// The next number of a counter in LDS, for the wavefront.
+__device__ __forceinline__ int few_draw(int *counter)
+{
+    int n = 0;
+    if (threadIdx.x % kWave == 0)
+        n = atomicAdd(counter, 1);
+    return __builtin_amdgcn_readfirstlane(n);
+}
+
+// Room in LDS for items whose parts are under way: how far wavefronts may be apart.
+struct FewRoom {
+    int parts_done[8]; // of the item in a place
+    int item[8];       // that may use a place
+};
+
+// Gate/up items of one class: (expert, `width` columns of F); a share's are `shares` apart.  A unit, which a wavefront draws,
+// is an item or one of `gate_parts` parts of its reduction.
 template <int kForm, int kTT>
 struct GateUp {
     using Form = FewForm<kForm>;
     static constexpr int kGate = kGateTiles<kForm>, kCT = 2 * kGate, kDepth = few_depth<kForm, kTT, kCT>();
-    static constexpr int kValues = kFewValues<kForm, kTT>;
+    static constexpr int kValues = kFewValues<kForm, kTT>, kPartFloats = kCT * kValues * kWave;
     const FewKernelArgs &g;
     const FewArgs &l;
     const FewLists &lists;
-    float *red; // [rounds held][wavefront][tile][value][lane]
-    int begin, items, first, rounds, lines, part_lines, tiles;
+    float *pool; // [place][part][tile][value][lane]
+    FewRoom &room;
+    int *counter;
+    int begin, items, first, mine, parts, places;
+    struct Unit {
+        int n, at, tile, part; // n-th item of the share
+    } open_unit, unit;
+    bool any = false;
 
-    // before: rounds of the classes before this one (rounds are numbered through all classes); it is moved on
-    __device__ GateUp(const FewKernelArgs &g, const FewLists &lists, float *red, int cls, int who, int &before)
-        : g(g), l(g.l), lists(lists), red(red), lines(g.h_lines), part_lines(g.part_lines), tiles(g.f_tiles)
+    // before: items of the classes before this one (items are numbered through all classes); it is moved on
+    __device__ GateUp(const FewKernelArgs &g, const FewLists &lists, float *pool, FewRoom &room, int *counter, int cls, int who, int &before)
+        : g(g), l(g.l), lists(lists), pool(pool), room(room), counter(counter), parts(g.gate_parts)
     {
         begin = __builtin_amdgcn_readfirstlane(lists.begin[cls]);
-        items = (__builtin_amdgcn_readfirstlane(lists.begin[cls + 1]) - begin) * tiles;
-        const int all = (items + kFewWaves / g.split - 1) / (kFewWaves / g.split);
+        items = (__builtin_amdgcn_readfirstlane(lists.begin[cls + 1]) - begin) * g.f_tiles;
         first = who - (before ? before % g.shares : 0);
         if (first < 0)
             first += g.shares;
-        rounds = first < all ? (all - 1 - first) / g.shares + 1 : 0;
-        before += all;
+        mine = first < items ? (items - 1 - first) / g.shares + 1 : 0;
+        before += items;
+        places = kPoolFloats / (parts * kPartFloats);
+        places = places < 8 ? places : 8;
     }
-    __device__ __forceinline__ int wave() const { return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); }
-    __device__ __forceinline__ int item_of(int round, int sub) const { return (first + round * g.shares) * (kFewWaves / g.split) + sub; }
-    __device__ __forceinline__ int segments() const { return rounds; }
-    __device__ __forceinline__ int groups(int) const { return (part_lines + kDepth - 1) / kDepth; }
-    __device__ __forceinline__ bool ready() const { return true; }
-    __device__ __forceinline__ void open(FewCursor<kForm, kTT, kCT, false> &c, int round)
+    __device__ __forceinline__ bool open(FewCursor<kForm, kTT, kCT, false> &c)
     {
-        const int item = item_of(round, wave() / g.split), part = wave() % g.split;
-        const bool there = item < items;
-        const int at = begin + (there ? item / tiles : 0), f0 = there ? item % tiles * g.width : 0;
+        const int u = few_draw(counter);
+        if (u >= mine * parts)
+            return false;
+        const int n = u / parts, item = first + n * g.shares, at = begin + item / g.f_tiles, f0 = item % g.f_tiles * g.width;
+        open_unit = {n, at, item % g.f_tiles, u % parts};
+        if (!any)
+            unit = open_unit;
+        any = true;
         const int expert = __builtin_amdgcn_readfirstlane(lists.expert[at]), base = __builtin_amdgcn_readfirstlane(lists.base[at]);
         const int rows = __builtin_amdgcn_readfirstlane(lists.rows[at]);
         const int64_t row = (int64_t)expert * l.F + f0, end = row + (l.F - f0 < g.width ? l.F - f0 : g.width);
@@ -291,93 +314,112 @@ struct GateUp {
         const uint32_t x_row = (uint32_t)l.H * Form::kElt;
         c.set_acts({static_cast<const unsigned char *>(l.x), (uint32_t)l.N * x_row, 0, 0, rows},
                    [&](int r) { return lists.token[base + r] * x_row; });
-        c.line = part * part_lines;
-        c.end = !there ? 0 : c.line + part_lines < lines ? c.line + part_lines : lines;
-        c.groups = groups(round);
+        c.line = g.h_lines * open_unit.part / parts;
+        c.end = g.h_lines * (open_unit.part + 1) / parts;
+        c.groups = c.end > c.line ? (c.end - c.line + kDepth - 1) / kDepth : 1;
+        return true;
     }
-    __device__ __forceinline__ void close(const FewSums<kForm, kTT, kCT> &sums, int round)
+    // Sixteen columns p, value v of the lanes.
+    __device__ __forceinline__ void store(int p, int v, float gate, float up) const
     {
-        const int lane = threadIdx.x % kWave;
-        float *const mine = red + round % kRoundsHeld<kForm, kTT> * kRoundFloats<kForm, kTT>;
-        if (kRoundsHeld<kForm, kTT> == 1)
-            few_barrier(); // the round before is read
+        const float a = silu_mul_f32(gate, up);
+        const int rows = __builtin_amdgcn_readfirstlane(lists.rows[unit.at]);
+        const FewActs to = few_activation<kForm>(g, lists, unit.at, rows);
+        const int r = few_row_of<kForm, kTT>(v), i = 16 * p + threadIdx.x % 16;
+        const bool there = r < rows && i < g.width && unit.tile * g.width + i < l.F;
+        unsigned char *const put = const_cast<unsigned char *>(to.data) + (int64_t)unit.tile * to.tile + (r * g.width + i) * Form::kElt;
+        if constexpr (kForm == kFewF32) {
+            if (there)
+                __hip_atomic_store(reinterpret_cast<uint32_t *>(put), __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        } else { // the even lane stores both columns (F and width are even)
+            const uint32_t both = pack_bf16x2(a, __shfl_xor(a, 1));
+            if (there && threadIdx.x % 2 == 0)
+                __hip_atomic_store(reinterpret_cast<uint32_t *>(put), both, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
+    __device__ __forceinline__ void close(const FewSums<kForm, kTT, kCT> &sums)
+    {
+        if (parts == 1) {
 #pragma unroll
-        for (int c = 0; c < kCT; ++c)
+            for (int p = 0; p < kGate; ++p)
 #pragma unroll
-            for (int v = 0; v < kValues; ++v)
-                mine[((wave() * kCT + c) * kValues + v) * kWave + lane] = sums.value(c, v);
-        few_barrier(); // (with room for two: the readers of the round before last were done before anyone came here)
-        // unit: sixteen columns of an item and a value of the lanes
-        const int units = kFewWaves / g.split * kGate * kValues;
-        for (int unit = (wave() + round) % kFewWaves; unit < units; unit += kFewWaves) {
-            const int sub = unit / (kGate * kValues), p = unit / kValues % kGate, v = unit % kValues, item = item_of(round, sub);
-            if (item >= items)
-                continue;
-            const float *from = mine + ((sub * g.split * kCT + p) * kValues + v) * kWave + lane;
-            float part[2][kFewWaves];
+                for (int v = 0; v < kValues; ++v)
+                    store(p, v, sums.value(p, v), sums.value(kGate + p, v));
+        } else {
+            // The item's place, once the item that had it before is done with; parts of older items never wait for younger ones.
+            const int lane = threadIdx.x % kWave, place = unit.n % places;
+            while (__builtin_amdgcn_readfirstlane(__hip_atomic_load(&room.item[place], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP)) != unit.n)
+                __builtin_amdgcn_s_sleep(1);
+            float *const slot = pool + place * parts * kPartFloats;
 #pragma unroll
-            for (int w = 0; w < kFewWaves; ++w) // (past the split: read for nothing, inside the round's sums all the same)
+            for (int c = 0; c < kCT; ++c)
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
-                    part[u][w] = from[((w < g.split ? w : 0) * kCT + u * kGate) * kValues * kWave];
-            float gate = part[0][0], up = part[1][0];
+                for (int v = 0; v < kValues; ++v)
+                    slot[unit.part * kPartFloats + (c * kValues + v) * kWave + lane] = sums.value(c, v);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // (LDS of a workgroup keeps its order)
+            if (few_draw(&room.parts_done[place]) == parts - 1) {
+                asm volatile("" ::: "memory");
+                for (int u = 0; u < kGate * kValues; ++u) {
+                    const int p = u / kValues, v = u % kValues;
+                    float part[2][8];
 #pragma unroll
-            for (int w = 1; w < kFewWaves; ++w) {
-                gate += w < g.split ? part[0][w] : 0.0f;
-                up += w < g.split ? part[1][w] : 0.0f;
-            }
-            const float a = silu_mul_f32(gate, up);
-            const int at = begin + item / tiles, tile = item % tiles;
-            const int rows = __builtin_amdgcn_readfirstlane(lists.rows[at]);
-            const FewActs to = few_activation<kForm>(g, lists, at, rows);
-            const int r = few_row_of<kForm, kTT>(v), i = 16 * p + lane % 16;
-            const bool there = r < rows && i < g.width && tile * g.width + i < l.F;
-            unsigned char *const put = const_cast<unsigned char *>(to.data) + (int64_t)tile * to.tile + (r * g.width + i) * Form::kElt;
-            if constexpr (kForm == kFewF32) {
-                if (there)
-                    __hip_atomic_store(reinterpret_cast<uint32_t *>(put), __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            } else { // the even lane stores both columns (F and width are even)
-                const uint32_t both = pack_bf16x2(a, __shfl_xor(a, 1));
-                if (there && lane % 2 == 0)
-                    __hip_atomic_store(reinterpret_cast<uint32_t *>(put), both, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    for (int w = 0; w < 8; ++w) // (past the last part: the first, for nothing)
+#pragma unroll
+                        for (int m = 0; m < 2; ++m)
+                            part[m][w] = slot[(w < parts ? w : 0) * kPartFloats + ((m * kGate + p) * kValues + v) * kWave + lane];
+                    float gate = part[0][0], up = part[1][0];
+#pragma unroll
+                    for (int w = 1; w < 8; ++w) {
+                        gate += w < parts ? part[0][w] : 0.0f;
+                        up += w < parts ? part[1][w] : 0.0f;
+                    }
+                    store(p, v, gate, up);
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                if (lane == 0) {
+                    room.parts_done[place] = 0;
+                    __hip_atomic_store(&room.item[place], unit.n + places, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                }
             }
         }
+        unit = open_unit;
     }
 };
 
-// A class's part of a down tile, columns [h0, h0 + cols): the experts' lines side by side are shared by the wavefronts, whose
-// weighted rows are added to their own sums per token.
-template <int kForm, int kTT, int kCT, class Ready>
+// A class's part of a down tile, columns [h0, h0 + cols).  A unit is one of `down_parts` parts of an expert's reduction; its
+// rows go to LDS by part and slot.
+template <int kForm, int kTT, int kCT>
 struct Down {
     using Form = FewForm<kForm>;
     static constexpr int kDepth = few_depth<kForm, kTT, kCT>();
     const FewKernelArgs &g;
     const FewArgs &l;
     const FewLists &lists;
-    float *token_sums;
+    float *pool; // [part][slot][16 kCT]
+    int *counter;
     int h0, cols;
-    Ready wait;
-    int lines, begin, from, to, first;
+    int begin, units;
+    struct Unit {
+        int at, part;
+    } open_unit, unit;
+    bool any = false;
 
-    __device__ Down(const FewKernelArgs &g, const FewLists &lists, float *token_sums, int cls, int h0, int cols, Ready wait)
-        : g(g), l(g.l), lists(lists), token_sums(token_sums), h0(h0), cols(cols), wait(wait)
+    __device__ Down(const FewKernelArgs &g, const FewLists &lists, float *pool, int *counter, int cls, int h0, int cols)
+        : g(g), l(g.l), lists(lists), pool(pool), counter(counter), h0(h0), cols(cols)
     {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-        lines = g.f_lines;
         begin = __builtin_amdgcn_readfirstlane(lists.begin[cls]);
-        const int64_t all = (int64_t)(__builtin_amdgcn_readfirstlane(lists.begin[cls + 1]) - begin) * lines;
-        from = (int)(all * wave / kFewWaves);
-        to = (int)(all * (wave + 1) / kFewWaves);
-        first = from / lines;
+        units = (__builtin_amdgcn_readfirstlane(lists.begin[cls + 1]) - begin) * g.down_parts;
     }
-    __device__ __forceinline__ int segments() const { return to > from ? (to - 1) / lines - first + 1 : 0; }
-    __device__ __forceinline__ int start_of(int k) const { return k ? (first + k) * lines : from; }
-    __device__ __forceinline__ int end_of(int k) const { return (first + k + 1) * lines < to ? (first + k + 1) * lines : to; }
-    __device__ __forceinline__ int groups(int k) const { return (end_of(k) - start_of(k) + kDepth - 1) / kDepth; }
-    __device__ __forceinline__ bool ready() { return wait(); }
-    __device__ __forceinline__ void open(FewCursor<kForm, kTT, kCT, true> &c, int k)
+    __device__ __forceinline__ bool open(FewCursor<kForm, kTT, kCT, true> &c)
     {
-        const int at = begin + first + k;
+        const int u = few_draw(counter);
+        if (u >= units)
+            return false;
+        const int at = begin + u / g.down_parts;
+        open_unit = {at, u % g.down_parts};
+        if (!any)
+            unit = open_unit;
+        any = true;
         const int expert = __builtin_amdgcn_readfirstlane(lists.expert[at]), rows = __builtin_amdgcn_readfirstlane(lists.rows[at]);
         const int64_t row = (int64_t)expert * l.H + h0, end = row + cols;
 #pragma unroll
@@ -385,25 +427,24 @@ struct Down {
             c.panel[p] = panel_of<kForm>(l.down, row + 16 * p, end, l.F, l.scale_cols_f);
         const uint32_t a_row = (uint32_t)g.width * Form::kElt;
         c.set_acts(few_activation<kForm>(g, lists, at, rows), [&](int r) { return r * a_row; });
-        c.line = start_of(k) - (first + k) * lines;
-        c.end = end_of(k) - (first + k) * lines;
-        c.groups = groups(k);
+        c.line = g.f_lines * open_unit.part / g.down_parts;
+        c.end = g.f_lines * (open_unit.part + 1) / g.down_parts;
+        c.groups = c.end > c.line ? (c.end - c.line + kDepth - 1) / kDepth : 1;
+        return true;
     }
-    __device__ __forceinline__ void close(const FewSums<kForm, kTT, kCT> &sums, int k)
+    __device__ __forceinline__ void close(const FewSums<kForm, kTT, kCT> &sums)
     {
-        const int at = begin + first + k;
-        const int base = __builtin_amdgcn_readfirstlane(lists.base[at]), rows = __builtin_amdgcn_readfirstlane(lists.rows[at]);
+        const int base = __builtin_amdgcn_readfirstlane(lists.base[unit.at]), rows = __builtin_amdgcn_readfirstlane(lists.rows[unit.at]);
+        float *const to = pool + (unit.part * l.N * l.K + base) * (16 * kCT) + threadIdx.x % 16;
 #pragma unroll
         for (int v = 0; v < kFewValues<kForm, kTT>; ++v) {
             const int r = few_row_of<kForm, kTT>(v);
-            if (r < rows) { // (a token has an expert once: the lanes of a wavefront meet nowhere)
-                const float w = lists.weight[base + r];
-                float *const to_sum = token_sums + lists.token[base + r] * (16 * kCT) + threadIdx.x % 16;
+            if (r < rows)
 #pragma unroll
                 for (int p = 0; p < kCT; ++p)
-                    to_sum[16 * p] += w * sums.value(p, v);
-            }
+                    to[r * (16 * kCT) + 16 * p] = sums.value(p, v);
         }
+        unit = open_unit;
     }
 };
 #endif
@@ -413,13 +454,13 @@ template <int kForm, int kMaxTT, int kCT>
 __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int kRed = kRoundFloats<kForm, kMaxTT> * kRoundsHeld<kForm, kMaxTT>, kSums = kFewWaves * 16 * kMaxTT * 16 * kCT;
     __shared__ union {
         FewRouting routing;
-        float red[kRed];
-        float sums[kSums];
+        float pool[kPoolFloats];
     } sh;
     __shared__ FewLists lists;
+    __shared__ FewRoom room;
+    __shared__ int counters[4]; // units drawn, of each class
     __shared__ int box[kFewWaves];
     const FewArgs &l = g.l;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -465,17 +506,30 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
 
     uint32_t *const share_flags = g.flags + 32;
     const FewCols in = {l.H, l.scale_cols_h, l.group}, mid = {l.F, l.scale_cols_f, l.group};
-    bool all_there = false;
+    auto restart = [&]() { // of the counters; everyone is done with them
+        if (threadIdx.x < 4)
+            counters[threadIdx.x] = 0;
+        if (threadIdx.x < 8) {
+            room.parts_done[threadIdx.x] = 0;
+            room.item[threadIdx.x] = threadIdx.x;
+        }
+        few_barrier();
+    };
+    auto empty = [&](int cls) { return __builtin_amdgcn_readfirstlane(lists.begin[cls]) == __builtin_amdgcn_readfirstlane(lists.begin[cls + 1]); };
     for (int who = blockIdx.x;;) {
         int before = 0;
+        restart();
         auto gate_up = [&](auto tt, int cls) {
             constexpr int kTT = decltype(tt)::value;
-            if (__builtin_amdgcn_readfirstlane(lists.begin[cls]) == __builtin_amdgcn_readfirstlane(lists.begin[cls + 1]))
+            if (empty(cls))
                 return;
             using Items = GateUp<kForm, kTT>;
-            Items items(g, lists, sh.red, cls, who, before);
+            Items items(g, lists, sh.pool, room, counters + cls, cls, who, before);
             few_stream<kForm, kTT, Items::kCT, Items::kDepth, false>(items, in);
-            few_barrier(); // (the next one writes red)
+            if (g.gate_parts > 1) { // the next class has other places in the pool
+                few_barrier();
+                restart();
+            }
         };
         gate_up(std::integral_constant<int, 0>{}, 0);
         gate_up(std::integral_constant<int, 1>{}, 1);
@@ -484,61 +538,54 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
             gate_up(std::integral_constant<int, 4>{}, 3);
         }
         few_signal(share_flags + who);
-
-        int missing = -1;
-        const int tile = l.N * 16 * kCT;
-        float *const mine = sh.sums + wave * tile;
-        for (int h0 = (int)blockIdx.x * g.down_cols; h0 < l.H && missing < 0; h0 += (int)gridDim.x * g.down_cols) {
-            for (int p = lane; p < tile; p += kWave)
-                mine[p] = 0.0f;
-            const int cols = l.H - h0 < g.down_cols ? l.H - h0 : g.down_cols;
-            auto wait = [&]() {
-                if (!all_there) {
-                    missing = few_missing(share_flags, g.shares, g.patience, box);
-                    all_there = missing < 0;
-                }
-                return all_there;
-            };
-            auto down = [&](auto tt, int cls) {
-                constexpr int kTT = decltype(tt)::value;
-                if (missing >= 0 || __builtin_amdgcn_readfirstlane(lists.begin[cls]) == __builtin_amdgcn_readfirstlane(lists.begin[cls + 1]))
-                    return;
-                using Part = Down<kForm, kTT, kCT, decltype(wait)>;
-                Part part(g, lists, mine, cls, h0, cols, wait);
-                few_stream<kForm, kTT, kCT, Part::kDepth, true>(part, mid);
-            };
-            down(std::integral_constant<int, 0>{}, 0);
-            down(std::integral_constant<int, 1>{}, 1);
-            if constexpr (kMaxTT > 1) {
-                down(std::integral_constant<int, 2>{}, 2);
-                down(std::integral_constant<int, 4>{}, 3);
-            }
-            if (missing >= 0)
-                break;
-            few_barrier();
-            for (int p = threadIdx.x * 2; p < tile; p += kFewThreads * 2) { // (columns are even)
-                float v[2];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    v[u] = sh.sums[p + u];
-#pragma unroll
-                    for (int w = 1; w < kFewWaves; ++w)
-                        v[u] += sh.sums[w * tile + p + u];
-                }
-                const int n = p / (16 * kCT), h = p % (16 * kCT);
-                if (h < cols) {
-                    if constexpr (kForm == kFewF32)
-                        *reinterpret_cast<f32x2 *>(static_cast<float *>(l.out) + (int64_t)n * l.H + h0 + h) = f32x2{v[0], v[1]};
-                    else
-                        *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(l.out) + (int64_t)n * l.H + h0 + h) = pack_bf16x2(v[0], v[1]);
-                }
-            }
-            few_barrier(); // (the sums are written again)
-        }
-        if (missing < 0)
+        if ((int)blockIdx.x * g.down_cols >= l.H)
             return;
+        who = few_missing(share_flags, g.shares, g.patience, box);
+        if (who < 0)
+            break;
+    }
+
+    for (int h0 = (int)blockIdx.x * g.down_cols; h0 < l.H; h0 += (int)gridDim.x * g.down_cols) {
+        const int cols = l.H - h0 < g.down_cols ? l.H - h0 : g.down_cols;
+        restart();
+        auto down = [&](auto tt, int cls) {
+            constexpr int kTT = decltype(tt)::value;
+            if (empty(cls))
+                return;
+            using Part = Down<kForm, kTT, kCT>;
+            Part part(g, lists, sh.pool, counters + cls, cls, h0, cols);
+            few_stream<kForm, kTT, kCT, Part::kDepth, true>(part, mid);
+        };
+        down(std::integral_constant<int, 0>{}, 0);
+        down(std::integral_constant<int, 1>{}, 1);
+        if constexpr (kMaxTT > 1) {
+            down(std::integral_constant<int, 2>{}, 2);
+            down(std::integral_constant<int, 4>{}, 3);
+        }
         few_barrier();
-        who = missing;
+        for (int p = threadIdx.x * 2; p < l.N * 16 * kCT; p += kFewThreads * 2) { // (columns are even)
+            const int n = p / (16 * kCT), h = p % (16 * kCT);
+            if (h >= cols)
+                continue;
+            float v[2] = {0.0f, 0.0f};
+            for (int k = 0; k < l.K; ++k) {
+                const float w = lists.weight[n * l.K + k];
+                const float *from = sh.pool + lists.slot[n * l.K + k] * (16 * kCT) + h;
+                float y[2] = {from[0], from[1]};
+                for (int part = 1; part < g.down_parts; ++part) {
+                    from += l.N * l.K * (16 * kCT);
+                    y[0] += from[0];
+                    y[1] += from[1];
+                }
+                v[0] += w * y[0];
+                v[1] += w * y[1];
+            }
+            if constexpr (kForm == kFewF32)
+                *reinterpret_cast<f32x2 *>(static_cast<float *>(l.out) + (int64_t)n * l.H + h0 + h) = f32x2{v[0], v[1]};
+            else
+                *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(l.out) + (int64_t)n * l.H + h0 + h) = pack_bf16x2(v[0], v[1]);
+        }
+        few_barrier(); // (the pool is written again)
     }
 #endif
 }

@@ -396,11 +396,9 @@ struct FewCursor {
 
 // A wavefront's stream: segment after segment (a panel of weight rows with the activation rows that meet it, some lines of
 // both), without a gap in the loads between them.  The source says what they are:
-//   segments()            how many
-//   groups(k)             of kDepth lines in segment k, at least 1 (lines past its end read as zeros)
-//   open(cursor, k)       sets the cursor to segment k; k ascending, a group ahead of
-//   close(sums, k)        takes the sums of segment k
-//   ready()               called once before the first load; false: the stream ends
+//   open(cursor)    sets the cursor to the next segment, with at least one group of kDepth lines (lines past its end read as
+//                   zeros); false: there is none.  A group ahead of
+//   close(sums)     takes the sums of the oldest open segment
 // A group is written out straight, so that what is waited for is the same on every path: segments change between groups only.
 // (With a change possible at every line the code is kDepth times as long, 180 KB, and waits for nearly everything in flight.)
 template <int kForm, int kTT, int kCT, int kDepth, bool kTiled, class Source>
@@ -409,14 +407,13 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
     using Form = FewForm<kForm>;
     using Ops = FewOperands<kForm, kTT, kCT>;
     using Cursor = FewCursor<kForm, kTT, kCT, kTiled>;
-    const int segments = source.segments();
-    if (!source.ready() || segments == 0)
+    Cursor c;
+    if (!source.open(c))
         return;
     const int i = threadIdx.x % kWave / 4, q = threadIdx.x % 4; // whose operand this lane fetches
     const uint32_t w_off = (uint32_t)i * (uint32_t)Form::row_bytes(g.cols) + (uint32_t)q * 16u;
     constexpr int kFours = Form::kQ4 ? (kDepth + 3) / 4 : 1; // scale loads per group of lines
     FewScales<kForm, kCT> scales[kFours];
-    Cursor c;
     auto fetch = [&](Ops &o) {
         const bool there = c.line < c.end; // (else no bytes: zeros, and the number of loads in flight stays)
 #pragma unroll
@@ -465,21 +462,21 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
         }
     };
     Ops o[kDepth];
-    int opened = 1;
-    source.open(c, 0);
+    int left = c.groups, next = 0; // groups of the segment that is multiplied, and of the one after it (0: there is none)
     fetch_scales();
 #pragma unroll
     for (int d = 0; d < kDepth; ++d)
         fetch(o[d]);
     FewSums<kForm, kTT, kCT> sums;
     sums.clear();
-    int closing = 0, left = source.groups(0);
     for (;;) {
         if (--c.groups == 0) { // the next group is another segment's
-            if (opened < segments)
-                source.open(c, opened++);
-            else
-                c.end = 0; // nothing more
+            if (source.open(c)) {
+                next = c.groups;
+            } else {
+                next = 0;
+                c.end = 0; // nothing more: no bytes
+            }
         }
         if constexpr (Form::kQ4) {
 #pragma unroll
@@ -495,11 +492,11 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
             fetch(o[d]);
         }
         if (--left == 0) {
-            source.close(sums, closing);
-            if (++closing == segments)
+            source.close(sums);
+            if (next == 0)
                 return;
             sums.clear();
-            left = source.groups(closing);
+            left = next;
         }
     }
 }
