@@ -39,8 +39,8 @@ namespace moe {
 constexpr int kFewWaves = 8, kFewThreads = kFewWaves * kWave;
 constexpr int kParts = 8; // partial sums of a logit between the launches
 constexpr int kRouteAll = 8;
-constexpr int kMaxRows = MOE_FEW_TOKENS * MOE_MAX_TOPK;
-constexpr int kTokenFlags = MOE_FEW_TOKENS / kFewWaves, kMaxShares = 1024, kFlags = 32 + kMaxShares; // tokens', then shares'
+constexpr int kMaxTokens = MOE_FEW_TOKENS, kMaxRows = kMaxTokens * (int)MOE_MAX_TOPK;
+constexpr int kMaxShares = 1024, kFlags = 32 + kMaxShares; // tokens', then shares'
 constexpr int kDefaultPatience = 1 << 15; // polls (about a microsecond each): longer than a share takes
 
 // ------------------------------------------------------------------------

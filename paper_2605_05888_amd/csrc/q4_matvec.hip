@@ -18,16 +18,17 @@ struct MatvecTile {
     int64_t m0;
     int rows;
     int64_t n0;
+    bool opened = false;
 
     __device__ __forceinline__ int lines() const { return (g.cols + Form::kLineCols - 1) / Form::kLineCols; }
     __device__ __forceinline__ int wave() const { return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); }
     __device__ __forceinline__ int first() const { return lines() * wave() / kMvWaves; }
     __device__ __forceinline__ int last() const { return lines() * (wave() + 1) / kMvWaves; }
-    __device__ __forceinline__ int segments() const { return 1; }
-    __device__ __forceinline__ int groups(int) const { return last() > first() ? (last() - first() + kDepth - 1) / kDepth : 1; }
-    __device__ __forceinline__ bool ready() const { return true; }
-    __device__ __forceinline__ void open(FewCursor<kForm, kTT, kCT, false> &c, int) const
+    __device__ __forceinline__ bool open(FewCursor<kForm, kTT, kCT, false> &c)
     {
+        if (opened)
+            return false;
+        opened = true;
         const int64_t row = (int64_t)e * g.rows + n0, end = (int64_t)(e + 1) * g.rows;
 #pragma unroll
         for (int p = 0; p < kCT; ++p)
@@ -37,9 +38,10 @@ struct MatvecTile {
                    [&](int r) { return r * x_row; });
         c.line = first();
         c.end = last();
-        c.groups = groups(0);
+        c.groups = last() > first() ? (last() - first() + kDepth - 1) / kDepth : 1;
+        return true;
     }
-    __device__ __forceinline__ void close(const FewSums<kForm, kTT, kCT> &sums, int) const
+    __device__ __forceinline__ void close(const FewSums<kForm, kTT, kCT> &sums) const
     {
         constexpr int kValues = kFewValues<kForm, kTT>;
         const int lane = threadIdx.x % kWave;
