@@ -421,8 +421,8 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
             const auto rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(c.panel[p].data), 0,
                                                               there ? (int)c.panel[p].bytes : 0, 0x00020000);
 #pragma unroll
-            for (int s = 0; s < Form::kLoads; ++s) // (weights are read once: non-temporal)
-                o.w[p][s] = __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(w_off + (uint32_t)(c.line * Form::kLineBytes + 64 * s)), 0, 2);
+            for (int s = 0; s < Form::kLoads; ++s)
+                o.w[p][s] = __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(w_off + (uint32_t)(c.line * Form::kLineBytes + 64 * s)), 0, 0);
         }
         const auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(c.act), 0, there ? (int)c.act_bytes : 0, 0x00020000);
 #pragma unroll
