@@ -57,6 +57,16 @@ constexpr uint32_t kNowhere = 0x40000000u; // an offset past every byte count us
 
 #if defined(__HIP_DEVICE_COMPILE__)
 
+// A buffer of `bytes` bytes at p.  Both are the same in all lanes; the compiler, which cannot see it everywhere, would else
+// load lane by lane in a loop.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t few_buffer(const void *p, uint32_t bytes)
+{
+    const uint64_t at = reinterpret_cast<uint64_t>(p);
+    const uint64_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at);
+    const uint64_t high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(high << 32 | low), 0, __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000);
+}
+
 // Sixteen weight rows.  bytes: of those that are there; scales: from the first row's first scale, scale_bytes as bytes.
 struct Panel {
     const unsigned char *data, *scales;
@@ -418,13 +428,12 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
         const bool there = c.line < c.end; // (else no bytes: zeros, and the number of loads in flight stays)
 #pragma unroll
         for (int p = 0; p < kCT; ++p) {
-            const auto rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(c.panel[p].data), 0,
-                                                              there ? (int)c.panel[p].bytes : 0, 0x00020000);
+            const auto rw = few_buffer(c.panel[p].data, there ? c.panel[p].bytes : 0u);
 #pragma unroll
             for (int s = 0; s < Form::kLoads; ++s)
                 o.w[p][s] = __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(w_off + (uint32_t)(c.line * Form::kLineBytes + 64 * s)), 0, 0);
         }
-        const auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(c.act), 0, there ? (int)c.act_bytes : 0, 0x00020000);
+        const auto ra = few_buffer(c.act, there ? c.act_bytes : 0u);
 #pragma unroll
         for (int t = 0; t < Ops::kActs; ++t) {
             const int col = c.line * Form::kLineCols + Cursor::chunk_col(kTT ? t : i % Form::kChunks);
@@ -446,8 +455,7 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
             for (int f = 0; f < kFours; ++f)
 #pragma unroll
                 for (int p = 0; p < kCT; ++p) {
-                    const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(c.panel[p].scales), 0,
-                                                                      c.line < c.end ? (int)c.panel[p].scale_bytes : 0, 0x00020000);
+                    const auto rs = few_buffer(c.panel[p].scales, c.line < c.end ? c.panel[p].scale_bytes : 0u);
                     const uint32_t want = (uint32_t)(i * g.scale_cols + (c.line + 4 * f + q) * per_line) * kBytes;
                     const uint32_t last = c.panel[p].scale_bytes - kLoad, at = want < last ? want : last;
                     scales[f].shift[p] = want - at < kLoad ? 8 * (want - at) : 0; // (further: of a row or line that is not there)
