@@ -117,16 +117,16 @@ size_t few_workspace_bytes(int64_t N, int64_t H, int E, int K, int64_t F, int dt
 // column per wavefront.  Narrow items make even shares of little work (one token, 4 experts of 1408 columns: 22 columns per
 // workgroup, three items of 8 or two of 16), wide ones use their loads and registers better; parts do the same for the
 // wavefronts of a workgroup, at the price of an exchange and of groups that are not full.
-static void choose_items(FewKernelArgs &g, double experts, int widest)
+static void choose_items(FewKernelArgs &g, double experts)
 {
     int64_t least = INT64_MAX;
-    for (int width = widest; width >= 8; width -= 8)
+    for (int width = 16; width >= 8; width -= 8)
         for (int parts = 1; parts <= kFewWaves && (parts == 1 || parts <= g.h_lines); parts *= 2) {
             const int64_t items = ceil_div((int64_t)(experts * (double)ceil_div(g.l.F, width) + 0.5), g.shares);
             const int64_t turns = ceil_div(items * parts, kFewWaves);
             const int64_t time = turns * (ceil_div(ceil_div(g.h_lines, parts), 4) * 4 * (width + 4) + (parts > 1 ? 40 : 20));
             if (time < least)
-                least = time, g.width = width, g.gate_parts = parts;
+                least = time, g.width = width;
         }
 }
 
@@ -146,7 +146,7 @@ int launch_layer_few(const FewArgs &args, int dtype, int format, hipStream_t st)
     const int rows = args.N * args.K;
     const double touched = args.E * (1.0 - pow(1.0 - (double)args.K / args.E, args.N)); // experts, if all are equally popular
     const double experts = touched < 1.0 ? 1.0 : touched;
-    choose_items(g, experts, format == MOE_Q4_FP4 ? 16 * kGateTiles<kFewFp4> : 16);
+    choose_items(g, experts);
     g.f_tiles = (int)ceil_div(args.F, g.width);
     // columns of a down tile: as many tiles as workgroups (or a multiple), none wider than 32, or 16 where the rows' sums would
     // not fit in LDS
@@ -166,8 +166,12 @@ int launch_layer_few(const FewArgs &args, int dtype, int format, hipStream_t st)
         hipLaunchKernelGGL(few_logits<false>, grid, dim3(2 * kWave), 0, st, args.x, args.N, args.H, args.W_r, args.E, w.parts, w.flags, kFlags);
     if (format == MOE_Q4_FP4)
         launch_few_ffn<kFewFp4>(g, st);
+    else if (format == MOE_Q4_INT4 && args.group == 32)
+        launch_few_ffn<kFewInt4By32>(g, st);
+    else if (format == MOE_Q4_INT4 && args.group == 64)
+        launch_few_ffn<kFewInt4By64>(g, st);
     else if (format == MOE_Q4_INT4)
-        launch_few_ffn<kFewInt4>(g, st);
+        launch_few_ffn<kFewInt4By128>(g, st);
     else if (dtype == MOE_BF16)
         launch_few_ffn<kFewBf16>(g, st);
     else

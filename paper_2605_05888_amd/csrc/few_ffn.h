@@ -24,7 +24,7 @@
 // its item was complete.  (Telling the caches to drop what they hold takes 5 - 9 us.)
 //
 // Rows of an expert are the set bits of a mask of 64 tokens: slot and count are population counts, in ascending n.  Experts are
-// taken in four classes by their rows (few_stream.h's forms), each a stream of its own.
+// taken in three classes by their rows (few_stream.h's forms), each a stream of its own.
 #pragma once
 
 #include <math.h>
@@ -36,7 +36,6 @@
 
 namespace moe {
 
-constexpr int kFewWaves = 8, kFewThreads = kFewWaves * kWave;
 constexpr int kParts = 8; // partial sums of a logit between the launches
 constexpr int kRouteAll = 8;
 constexpr int kMaxTokens = MOE_FEW_TOKENS, kMaxRows = kMaxTokens * (int)MOE_MAX_TOPK;
@@ -49,17 +48,12 @@ struct FewKernelArgs {
     const float *parts;
     uint32_t *flags;
     int shares;    // of gate/up items
-    int width;      // columns of F of an item: a multiple of 8, at most 16 * kGateTiles
-    int gate_parts; // of an item's reduction: 1, 2, 4 or 8
+    int width;      // columns of F of an item: 8 or 16
     int down_cols;  // columns of H of a down tile, at most 16 kCT
     int down_parts; // of an expert's reduction there
     int patience;
     int h_lines, f_lines, f_tiles; // lines of H and F; items of an expert
 };
-
-// Sixteens of columns of a gate/up item, each of both matrices.
-template <int kForm>
-constexpr int kGateTiles = kForm == kFewFp4 ? 2 : 1;
 
 constexpr int kPoolFloats = 32768; // LDS for partial sums
 
@@ -88,12 +82,14 @@ __device__ __forceinline__ Pick few_select(const FewKernelArgs &g, int n)
                               : select_top<MOE_MAX_EXPERTS / kWave>(logit_of, l.E, l.K, l.score_mode);
 }
 
-// The experts that got a row, by class and in ascending order within it, and their rows: slots from base on.
+// The experts that got a row, by class and in ascending order within it, and their rows: slots from base on.  An expert with
+// more than a stream's rows (N K / 33 experts at most) is there twice: with that many, and with the rest.
+constexpr int kMaxEntries = MOE_MAX_EXPERTS + kMaxRows / 33;
 struct FewLists {
-    int begin[5]; // of the classes: at most kFewRows rows, 16, 32, 64
-    uint16_t expert[MOE_MAX_EXPERTS], base[MOE_MAX_EXPERTS];
-    uint16_t lines[MOE_MAX_EXPERTS]; // cache lines of one activation tile before this expert's
-    uint8_t rows[MOE_MAX_EXPERTS];
+    int begin[4]; // of the classes: at most kFewRows rows, 16, 32
+    uint16_t expert[kMaxEntries], base[kMaxEntries];
+    uint16_t lines[kMaxEntries]; // cache lines of one activation tile before this one's
+    uint8_t rows[kMaxEntries];
     uint8_t token[kMaxRows]; // of a slot
     uint16_t slot[kMaxRows]; // of n * K + k, and its weight
     float weight[kMaxRows];
@@ -124,15 +120,16 @@ __device__ __forceinline__ void few_make_lists(FewLists &lists, FewRouting &r, i
     __syncthreads();
     // Two experts per thread.  Sums: cache lines of a tile in the low 13 bits, then experts of each class in 11 bits; slots.
     constexpr int kPer = MOE_MAX_EXPERTS / kFewThreads;
-    auto shift_of = [](int rows) { return 13 + 11 * (rows <= FewForm<kForm>::kFewRows ? 0 : rows <= 16 ? 1 : rows <= 32 ? 2 : 3); };
+    auto shift_of = [](int rows) { return 13 + 11 * (rows <= FewForm<kForm>::kFewRows ? 0 : rows <= 16 ? 1 : 2); };
     uint64_t mine[kPer], up_to = 0;
     uint32_t slots = 0;
     int rows[kPer];
+    auto entry = [&](int rows) { return rows ? (uint64_t)few_tile_lines<kForm>(rows, width) | 1ull << shift_of(rows) : 0; };
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int e = threadIdx.x * kPer + i;
         rows[i] = e < E ? (int)__popcll(r.mask[e]) : 0;
-        mine[i] = rows[i] ? (uint64_t)few_tile_lines<kForm>(rows[i], width) | 1ull << shift_of(rows[i]) : 0;
+        mine[i] = rows[i] <= kFewMost ? entry(rows[i]) : entry(kFewMost) + entry(rows[i] - kFewMost);
         up_to += mine[i];
         slots += rows[i];
     }
@@ -158,26 +155,32 @@ __device__ __forceinline__ void few_make_lists(FewLists &lists, FewRouting &r, i
         slot += w < wave ? r.wave_rows[w] : 0u;
         all += r.wave_sum[w];
     }
-    int begin[5] = {0, 0, 0, 0, 0};
+    int begin[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+    for (int c = 0; c < 3; ++c)
         begin[c + 1] = begin[c] + (int)(all >> (13 + 11 * c) & 0x7FF);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        if (rows[i]) {
-            const int e = threadIdx.x * kPer + i, shift = shift_of(rows[i]);
-            const int place = (shift == 13 ? 0 : shift == 24 ? begin[1] : shift == 35 ? begin[2] : begin[3]) + (int)(at >> shift & 0x7FF);
+        const int e = threadIdx.x * kPer + i;
+        uint64_t here = at;
+        for (int done = 0; done < rows[i];) {
+            const int some = rows[i] - done < kFewMost ? rows[i] - done : kFewMost, shift = shift_of(some);
+            const int place = (shift == 13 ? 0 : shift == 24 ? begin[1] : begin[2]) + (int)(here >> shift & 0x7FF);
             lists.expert[place] = (uint16_t)e;
-            lists.rows[place] = (uint8_t)rows[i];
-            lists.lines[place] = (uint16_t)(at & 0x1FFF);
-            lists.base[place] = r.first[e] = (uint16_t)slot;
+            lists.rows[place] = (uint8_t)some;
+            lists.lines[place] = (uint16_t)(here & 0x1FFF);
+            lists.base[place] = (uint16_t)(slot + done);
+            here += entry(some);
+            done += some;
         }
+        if (rows[i])
+            r.first[e] = (uint16_t)slot;
         at += mine[i];
         slot += rows[i];
     }
     if (threadIdx.x == 0)
 #pragma unroll
-        for (int c = 0; c < 5; ++c)
+        for (int c = 0; c < 4; ++c)
             lists.begin[c] = begin[c];
     __syncthreads();
     for (int p = threadIdx.x; p < N * K; p += kFewThreads) {
@@ -227,15 +230,6 @@ __device__ __forceinline__ void few_signal(uint32_t *flag)
         __hip_atomic_store(flag, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// Lines in flight per wavefront: what 256 registers hold beside a line's products (registers of a line in the comment).
-template <int kForm, int kTT, int kCT>
-constexpr int few_depth()
-{
-    if (FewForm<kForm>::kQ4) // 4 kCT + 4, 16, 32, 64
-        return kCT <= 2 && kTT == 0 ? 8 : kTT <= 1 ? 4 : kTT == 4 && kCT == 4 ? 1 : 2;
-    return kTT <= 1 ? (kCT == 1 ? 8 : 4) : kTT == 2 ? 4 : 2; // 8 kCT + 4, 8, 16, 32
-}
-
 // The activation of the expert at place `at`.
 template <int kForm>
 __device__ __forceinline__ FewActs few_activation(const FewKernelArgs &g, const FewLists &lists, int at, int rows)
@@ -245,35 +239,20 @@ __device__ __forceinline__ FewActs few_activation(const FewKernelArgs &g, const 
     return {static_cast<const unsigned char *>(g.l.a) + (int64_t)lines * tiles * 128, tiles * tile, g.width, tile, rows};
 }
 
-// The next number of a counter in LDS, for the wavefront.
-__device__ __forceinline__ int few_draw(int *counter)
-{
-    int n = 0;
-    if (threadIdx.x % kWave == 0)
-        n = atomicAdd(counter, 1);
-    return __builtin_amdgcn_readfirstlane(n);
-}
-
-// Room in LDS for items whose parts are under way: how far wavefronts may be apart.
-struct FewRoom {
-    int parts_done[8]; // of the item in a place
-    int item[8];       // that may use a place
-};
-
 // Gate/up items of one class: (expert, `width` columns of F); a share's are `shares` apart.  A unit, which a wavefront draws,
-// is an item or one of `gate_parts` parts of its reduction.
+// is an item or a part of its reduction.
 template <int kForm, int kTT>
 struct GateUp {
     using Form = FewForm<kForm>;
-    static constexpr int kGate = kGateTiles<kForm>, kCT = 2 * kGate, kDepth = few_depth<kForm, kTT, kCT>();
-    static constexpr int kValues = kFewValues<kForm, kTT>, kPartFloats = kCT * kValues * kWave;
+    static constexpr int kCT = 2, kDepth = few_depth<kForm, kTT, kCT>(); // tiles: gate, up
+    static constexpr int kValues = kFewValues<kForm, kTT>;
     const FewKernelArgs &g;
     const FewArgs &l;
     const FewLists &lists;
-    float *pool; // [place][part][tile][value][lane]
+    float *pool;
     FewRoom &room;
     int *counter;
-    int begin, items, first, mine, parts, places;
+    int begin, items, first, mine, parts;
     struct Unit {
         int n, at, tile, part; // n-th item of the share
     } open_unit, unit;
@@ -281,7 +260,7 @@ struct GateUp {
 
     // before: items of the classes before this one (items are numbered through all classes); it is moved on
     __device__ GateUp(const FewKernelArgs &g, const FewLists &lists, float *pool, FewRoom &room, int *counter, int cls, int who, int &before)
-        : g(g), l(g.l), lists(lists), pool(pool), room(room), counter(counter), parts(g.gate_parts)
+        : g(g), l(g.l), lists(lists), pool(pool), room(room), counter(counter)
     {
         begin = __builtin_amdgcn_readfirstlane(lists.begin[cls]);
         items = (__builtin_amdgcn_readfirstlane(lists.begin[cls + 1]) - begin) * g.f_tiles;
@@ -290,8 +269,7 @@ struct GateUp {
             first += g.shares;
         mine = first < items ? (items - 1 - first) / g.shares + 1 : 0;
         before += items;
-        places = kPoolFloats / (parts * kPartFloats);
-        places = places < 8 ? places : 8;
+        parts = __builtin_amdgcn_readfirstlane(few_parts(mine, g.h_lines, kDepth));
     }
     __device__ __forceinline__ bool open(FewCursor<kForm, kTT, kCT, false> &c)
     {
@@ -306,11 +284,8 @@ struct GateUp {
         const int expert = __builtin_amdgcn_readfirstlane(lists.expert[at]), base = __builtin_amdgcn_readfirstlane(lists.base[at]);
         const int rows = __builtin_amdgcn_readfirstlane(lists.rows[at]);
         const int64_t row = (int64_t)expert * l.F + f0, end = row + (l.F - f0 < g.width ? l.F - f0 : g.width);
-#pragma unroll
-        for (int p = 0; p < kGate; ++p) {
-            c.panel[p] = panel_of<kForm>(l.gate, row + 16 * p, end, l.H, l.scale_cols_h);
-            c.panel[kGate + p] = panel_of<kForm>(l.up, row + 16 * p, end, l.H, l.scale_cols_h);
-        }
+        c.panel[0] = panel_of<kForm>(l.gate, row, end, l.H, l.scale_cols_h);
+        c.panel[1] = panel_of<kForm>(l.up, row, end, l.H, l.scale_cols_h);
         const uint32_t x_row = (uint32_t)l.H * Form::kElt;
         c.set_acts({static_cast<const unsigned char *>(l.x), (uint32_t)l.N * x_row, 0, 0, rows},
                    [&](int r) { return lists.token[base + r] * x_row; });
@@ -319,13 +294,13 @@ struct GateUp {
         c.groups = c.end > c.line ? (c.end - c.line + kDepth - 1) / kDepth : 1;
         return true;
     }
-    // Sixteen columns p, value v of the lanes.
-    __device__ __forceinline__ void store(int p, int v, float gate, float up) const
+    // Value v of the lanes.
+    __device__ __forceinline__ void store(int v, float gate, float up) const
     {
         const float a = silu_mul_f32(gate, up);
         const int rows = __builtin_amdgcn_readfirstlane(lists.rows[unit.at]);
         const FewActs to = few_activation<kForm>(g, lists, unit.at, rows);
-        const int r = few_row_of<kForm, kTT>(v), i = 16 * p + threadIdx.x % 16;
+        const int r = few_row_of<kForm, kTT>(v), i = threadIdx.x % 16;
         const bool there = r < rows && i < g.width && unit.tile * g.width + i < l.F;
         unsigned char *const put = const_cast<unsigned char *>(to.data) + (int64_t)unit.tile * to.tile + (r * g.width + i) * Form::kElt;
         if constexpr (kForm == kFewF32) {
@@ -341,46 +316,13 @@ struct GateUp {
     {
         if (parts == 1) {
 #pragma unroll
-            for (int p = 0; p < kGate; ++p)
-#pragma unroll
-                for (int v = 0; v < kValues; ++v)
-                    store(p, v, sums.value(p, v), sums.value(kGate + p, v));
+            for (int v = 0; v < kValues; ++v)
+                store(v, sums.value(0, v), sums.value(1, v));
         } else {
-            // The item's place, once the item that had it before is done with; parts of older items never wait for younger ones.
-            const int lane = threadIdx.x % kWave, place = unit.n % places;
-            while (__builtin_amdgcn_readfirstlane(__hip_atomic_load(&room.item[place], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP)) != unit.n)
-                __builtin_amdgcn_s_sleep(1);
-            float *const slot = pool + place * parts * kPartFloats;
-#pragma unroll
-            for (int c = 0; c < kCT; ++c)
-#pragma unroll
+            FewJoin<kForm, kTT, kCT>(pool, kPoolFloats, room, parts).close(sums, unit.n, unit.part, [&](auto total) {
                 for (int v = 0; v < kValues; ++v)
-                    slot[unit.part * kPartFloats + (c * kValues + v) * kWave + lane] = sums.value(c, v);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // (LDS of a workgroup keeps its order)
-            if (few_draw(&room.parts_done[place]) == parts - 1) {
-                asm volatile("" ::: "memory");
-                for (int u = 0; u < kGate * kValues; ++u) {
-                    const int p = u / kValues, v = u % kValues;
-                    float part[2][8];
-#pragma unroll
-                    for (int w = 0; w < 8; ++w) // (past the last part: the first, for nothing)
-#pragma unroll
-                        for (int m = 0; m < 2; ++m)
-                            part[m][w] = slot[(w < parts ? w : 0) * kPartFloats + ((m * kGate + p) * kValues + v) * kWave + lane];
-                    float gate = part[0][0], up = part[1][0];
-#pragma unroll
-                    for (int w = 1; w < 8; ++w) {
-                        gate += w < parts ? part[0][w] : 0.0f;
-                        up += w < parts ? part[1][w] : 0.0f;
-                    }
-                    store(p, v, gate, up);
-                }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                if (lane == 0) {
-                    room.parts_done[place] = 0;
-                    __hip_atomic_store(&room.item[place], unit.n + places, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                }
-            }
+                    store(v, total(0, v), total(1, v));
+            });
         }
         unit = open_unit;
     }
@@ -449,7 +391,7 @@ struct Down {
 };
 #endif
 
-// kMaxTT: sixteens of rows that an expert can have (N).  kCT: sixteens of columns of a down tile.
+// kMaxTT: sixteens of rows that an entry of the lists can have.  kCT: sixteens of columns of a down tile.
 template <int kForm, int kMaxTT, int kCT>
 __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
 {
@@ -460,7 +402,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
     } sh;
     __shared__ FewLists lists;
     __shared__ FewRoom room;
-    __shared__ int counters[4]; // units drawn, of each class
+    __shared__ int counters[3]; // units drawn, of each class
     __shared__ int box[kFewWaves];
     const FewArgs &l = g.l;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -505,9 +447,9 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
     few_make_lists<kForm>(lists, sh.routing, l.N, l.K, l.E, g.width);
 
     uint32_t *const share_flags = g.flags + 32;
-    const FewCols in = {l.H, l.scale_cols_h, l.group}, mid = {l.F, l.scale_cols_f, l.group};
+    const FewCols in = {l.H, l.scale_cols_h}, mid = {l.F, l.scale_cols_f};
     auto restart = [&]() { // of the counters; everyone is done with them
-        if (threadIdx.x < 4)
+        if (threadIdx.x < 3)
             counters[threadIdx.x] = 0;
         if (threadIdx.x < 8) {
             room.parts_done[threadIdx.x] = 0;
@@ -526,17 +468,15 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
             using Items = GateUp<kForm, kTT>;
             Items items(g, lists, sh.pool, room, counters + cls, cls, who, before);
             few_stream<kForm, kTT, Items::kCT, Items::kDepth, false>(items, in);
-            if (g.gate_parts > 1) { // the next class has other places in the pool
+            if (items.parts > 1) { // (the next class has other places in the pool)
                 few_barrier();
                 restart();
             }
         };
         gate_up(std::integral_constant<int, 0>{}, 0);
         gate_up(std::integral_constant<int, 1>{}, 1);
-        if constexpr (kMaxTT > 1) {
+        if constexpr (kMaxTT > 1)
             gate_up(std::integral_constant<int, 2>{}, 2);
-            gate_up(std::integral_constant<int, 4>{}, 3);
-        }
         few_signal(share_flags + who);
         if ((int)blockIdx.x * g.down_cols >= l.H)
             return;
@@ -558,10 +498,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
         };
         down(std::integral_constant<int, 0>{}, 0);
         down(std::integral_constant<int, 1>{}, 1);
-        if constexpr (kMaxTT > 1) {
+        if constexpr (kMaxTT > 1)
             down(std::integral_constant<int, 2>{}, 2);
-            down(std::integral_constant<int, 4>{}, 3);
-        }
         few_barrier();
         for (int p = threadIdx.x * 2; p < l.N * 16 * kCT; p += kFewThreads * 2) { // (columns are even)
             const int n = p / (16 * kCT), h = p % (16 * kCT);
@@ -601,15 +539,17 @@ void launch_few_ffn(const FewKernelArgs &g, hipStream_t st)
             hipLaunchKernelGGL((few_ffn<kForm, 1, 2>), grid, block, 0, st, g);
     } else {
         if (g.down_cols <= 16)
-            hipLaunchKernelGGL((few_ffn<kForm, 4, 1>), grid, block, 0, st, g);
+            hipLaunchKernelGGL((few_ffn<kForm, 2, 1>), grid, block, 0, st, g);
         else
-            hipLaunchKernelGGL((few_ffn<kForm, 4, 2>), grid, block, 0, st, g);
+            hipLaunchKernelGGL((few_ffn<kForm, 2, 2>), grid, block, 0, st, g);
     }
 }
 
 extern template void launch_few_ffn<kFewBf16>(const FewKernelArgs &g, hipStream_t st);
 extern template void launch_few_ffn<kFewF32>(const FewKernelArgs &g, hipStream_t st);
 extern template void launch_few_ffn<kFewFp4>(const FewKernelArgs &g, hipStream_t st);
-extern template void launch_few_ffn<kFewInt4>(const FewKernelArgs &g, hipStream_t st);
+extern template void launch_few_ffn<kFewInt4By32>(const FewKernelArgs &g, hipStream_t st);
+extern template void launch_few_ffn<kFewInt4By64>(const FewKernelArgs &g, hipStream_t st);
+extern template void launch_few_ffn<kFewInt4By128>(const FewKernelArgs &g, hipStream_t st);
 
 }  // namespace moe

@@ -38,11 +38,13 @@
 namespace moe {
 
 // How a weight matrix is held; activations are bf16 but for kFewF32.
-enum { kFewBf16 = 0, kFewF32 = 1, kFewFp4 = 2, kFewInt4 = 3 };
+// (INT4: by the columns of a scale.)
+enum { kFewBf16 = 0, kFewF32 = 1, kFewFp4 = 2, kFewInt4By32 = 3, kFewInt4By64 = 4, kFewInt4By128 = 5 };
 
 template <int kForm>
 struct FewForm {
-    static constexpr bool kQ4 = kForm == kFewFp4 || kForm == kFewInt4;
+    static constexpr bool kInt4 = kForm >= kFewInt4By32, kQ4 = kForm == kFewFp4 || kInt4;
+    static constexpr int kSame = kForm == kFewInt4By128 ? 4 : kForm == kFewInt4By64 ? 2 : 1; // groups of 32 columns under one scale
     static constexpr int kElt = kForm == kFewF32 ? 4 : 2;                        // bytes of an activation
     static constexpr int kLineCols = kQ4 ? 128 : kForm == kFewF32 ? 32 : 64;     // columns of a line
     static constexpr int kLineBytes = kQ4 ? 64 : 128;                            // of a weight row
@@ -53,6 +55,8 @@ struct FewForm {
     __host__ __device__ static constexpr int64_t row_bytes(int64_t cols) { return kQ4 ? cols / 2 : cols * kElt; }
 };
 
+constexpr int kFewWaves = 8, kFewThreads = kFewWaves * kWave; // of a workgroup
+constexpr int kFewMost = 32; // rows of a stream: what 256 registers hold
 constexpr uint32_t kNowhere = 0x40000000u; // an offset past every byte count used here, twice too: loads give zeros
 
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -92,8 +96,8 @@ __device__ __forceinline__ Panel panel_of(const FewMatrix &w, int64_t row, int64
     return p;
 }
 
-// Where the activations of a segment are.  Row-major (width 0): rows at row_of(r).  Else tiles of `width` columns (8, 16, 24 or 32), `tile` bytes apart, and in a tile the rows
-// at row_of(r).  All below `bytes`.
+// Where the activations of a segment are, all below `bytes`.  Row-major (width 0): rows at row_of(r).  Else tiles of `width`
+// columns (8 or 16), `tile` bytes apart, and in a tile the rows at row_of(r).
 struct FewActs {
     const unsigned char *data;
     uint32_t bytes;
@@ -104,7 +108,6 @@ struct FewActs {
 
 struct FewCols {
     int cols, scale_cols;
-    int group; // of INT4
 };
 
 // Values a lane ends up with per weight row, and the activation row of value v.
@@ -127,7 +130,7 @@ struct FewOperands {
 template <int kForm, int kTT, int kCT>
 struct FewSums {
     static constexpr int kRows = kTT ? kTT : 1;
-    static constexpr bool kScalar = kForm == kFewInt4 && kTT == 0;
+    static constexpr bool kScalar = FewForm<kForm>::kInt4 && kTT == 0;
     static constexpr int kParts = kTT ? 1 : FewForm<kForm>::kChunks;
     f32x4 acc[kScalar ? 1 : kRows][kScalar ? 1 : kCT][kScalar ? 1 : kParts];
     float one[kScalar ? kCT : 1];
@@ -200,7 +203,7 @@ __device__ __forceinline__ u32x4 transpose_quads(u32x4 w)
 // Scales of four lines: as loaded (lane q: those of line q, FP4 four bytes, INT4 up to four bf16), and for every lane.
 template <int kForm, int kCT>
 struct FewScales {
-    static constexpr int kRegs = kForm == kFewInt4 ? 2 : 1;
+    static constexpr int kRegs = kForm == kFewInt4By32 ? 2 : 1;
     uint32_t raw[kCT][kRegs];
     uint32_t shift[kCT]; // bits that a load was moved back by, so as not to pass the panel's end
     uint32_t of[kCT][4][kRegs];
@@ -210,7 +213,7 @@ struct FewScales {
         const int row = (int)(threadIdx.x % 16) * 16; // byte address of the lane that fetched line 0's of row i
 #pragma unroll
         for (int c = 0; c < kCT; ++c) {
-            if constexpr (kForm == kFewInt4) {
+            if constexpr (kRegs == 2) {
                 const uint64_t v = ((uint64_t)raw[c][1] << 32 | raw[c][0]) >> (shift[c] & 63);
                 raw[c][0] = (uint32_t)v, raw[c][1] = (uint32_t)(v >> 32);
             } else {
@@ -241,24 +244,29 @@ __device__ __forceinline__ void to_operand_lane(u32x4 &v)
         v[j] = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)v[j]);
 }
 
+template <int kForm, int kTT, int kCT>
+__device__ __forceinline__ void to_operand_lanes(FewOperands<kForm, kTT, kCT> &o)
+{
+#pragma unroll
+    for (int c = 0; c < kCT; ++c)
+#pragma unroll
+        for (int l = 0; l < FewForm<kForm>::kLoads; ++l)
+            to_operand_lane(o.w[c][l]);
+#pragma unroll
+    for (int m = 0; m < FewOperands<kForm, kTT, kCT>::kRows; ++m)
+#pragma unroll
+        for (int t = 0; t < FewOperands<kForm, kTT, kCT>::kActs; ++t)
+            to_operand_lane(o.a[m][t]);
+}
+
 // Line d of four.
 template <int kForm, int kTT, int kCT>
-__device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, FewOperands<kForm, kTT, kCT> &o,
-                                             const FewScales<kForm, kCT> &scales, int d, int group)
+__device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, const FewOperands<kForm, kTT, kCT> &o,
+                                             const FewScales<kForm, kCT> &scales, int d)
 {
     using Form = FewForm<kForm>;
     using Ops = FewOperands<kForm, kTT, kCT>;
     const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int c = 0; c < kCT; ++c)
-#pragma unroll
-        for (int l = 0; l < Form::kLoads; ++l)
-            to_operand_lane(o.w[c][l]);
-#pragma unroll
-    for (int m = 0; m < Ops::kRows; ++m)
-#pragma unroll
-        for (int t = 0; t < Ops::kActs; ++t)
-            to_operand_lane(o.a[m][t]);
     if constexpr (kForm == kFewF32) {
 #pragma unroll
         for (int t = 0; t < Form::kChunks; ++t)
@@ -272,17 +280,19 @@ __device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, Few
                         acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(o.a[m][kTT ? t : 0][j]),
                                                                    __uint_as_float(o.w[c][t][j]), acc, 0, 0, 0);
                 }
-    } else if constexpr (kForm != kFewInt4) {
+    } else if constexpr (!Form::kInt4) {
+        u32x4 codes[kCT];
+        if constexpr (kForm == kFewFp4)
 #pragma unroll
-        for (int c = 0; c < kCT; ++c) {
-            u32x4 codes;
-            if constexpr (kForm == kFewFp4)
-                codes = transpose_quads(o.w[c][0]);
+            for (int c = 0; c < kCT; ++c)
+                codes[c] = transpose_quads(o.w[c][0]);
 #pragma unroll
-            for (int t = 0; t < Form::kChunks; ++t) {
+        for (int t = 0; t < Form::kChunks; ++t)
+#pragma unroll
+            for (int c = 0; c < kCT; ++c) {
                 bf16x8 w;
                 if constexpr (kForm == kFewFp4)
-                    w = fp4_operand(codes[t], scales.fp4(c, d, t));
+                    w = fp4_operand(codes[c][t], scales.fp4(c, d, t));
                 else
                     w = __builtin_bit_cast(bf16x8, o.w[c][t]);
 #pragma unroll
@@ -291,13 +301,12 @@ __device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, Few
                     acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, o.a[m][kTT ? t : 0]), w, acc, 0, 0, 0);
                 }
             }
-        }
     } else {
+        constexpr int kSame = Form::kSame;
         const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
         if constexpr (kTT == 0) {
             const bf16x8 a = int4_order(o.a[0][0]);
             const f32x4 sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, ones, zero, 0, 0, 0);
-            const int shift = group == 32 ? 0 : group == 64 ? 1 : 2;
 #pragma unroll
             for (int c = 0; c < kCT; ++c) {
                 const u32x4 codes = transpose_quads(o.w[c][0]);
@@ -307,15 +316,13 @@ __device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, Few
                     const f32x4 p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, int4_operand(codes[t]), zero, 0, 0, 0);
                     v[t] = fmaf(-136.0f, sum[t], p[t]);
                 }
-                if (shift == 0) {
 #pragma unroll
-                    for (int t = 0; t < 4; ++t)
-                        sums.one[c] = fmaf(scales.int4(c, d, t), v[t], sums.one[c]);
-                } else if (shift == 1) {
-                    sums.one[c] = fmaf(scales.int4(c, d, 0), v[0] + v[1], sums.one[c]);
-                    sums.one[c] = fmaf(scales.int4(c, d, 1), v[2] + v[3], sums.one[c]);
-                } else {
-                    sums.one[c] = fmaf(scales.int4(c, d, 0), (v[0] + v[1]) + (v[2] + v[3]), sums.one[c]);
+                for (int t = 0; t < 4; t += kSame) {
+                    float all = v[t];
+#pragma unroll
+                    for (int u = 1; u < kSame; ++u)
+                        all += v[t + u];
+                    sums.one[c] = fmaf(scales.int4(c, d, t / kSame), all, sums.one[c]);
                 }
                 __builtin_amdgcn_sched_barrier(0); // (else the products of all tiles are alive at once)
             }
@@ -324,39 +331,38 @@ __device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, Few
 #pragma unroll
             for (int c = 0; c < kCT; ++c)
                 codes[c] = transpose_quads(o.w[c][0]);
-            auto chained = [&](auto groups) { // of 32 columns under one scale
-                constexpr int kSame = decltype(groups)::value;
 #pragma unroll
-                for (int t = 0; t < 4; t += kSame)
+            for (int t = 0; t < 4; t += kSame) {
+                bf16x8 w[kCT][kSame];
 #pragma unroll
-                    for (int m = 0; m < Ops::kRows; ++m) {
-                        bf16x8 a[kSame];
-                        f32x4 sum = zero;
+                for (int c = 0; c < kCT; ++c)
 #pragma unroll
-                        for (int u = 0; u < kSame; ++u) {
-                            a[u] = int4_order(o.a[m][kTT ? t + u : 0]);
-                            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[u], ones, sum, 0, 0, 0);
-                        }
+                    for (int u = 0; u < kSame; ++u)
+                        w[c][u] = int4_operand(codes[c][t + u]);
 #pragma unroll
-                        for (int c = 0; c < kCT; ++c) {
-                            f32x4 p = zero;
+                for (int m = 0; m < Ops::kRows; ++m) {
+                    f32x4 sum = zero, p[kCT];
 #pragma unroll
-                            for (int u = 0; u < kSame; ++u)
-                                p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[u], int4_operand(codes[c][t + u]), p, 0, 0, 0);
-                            const float scale = scales.int4(c, d, t / kSame);
+                    for (int c = 0; c < kCT; ++c)
+                        p[c] = zero;
 #pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                sums.acc[m][c][0][r] = fmaf(scale, fmaf(-136.0f, sum[r], p[r]), sums.acc[m][c][0][r]);
-                        }
-                        __builtin_amdgcn_sched_barrier(0);
+                    for (int u = 0; u < kSame; ++u) {
+                        const bf16x8 a = int4_order(o.a[m][kTT ? t + u : 0]);
+                        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, ones, sum, 0, 0, 0);
+#pragma unroll
+                        for (int c = 0; c < kCT; ++c)
+                            p[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[c][u], p[c], 0, 0, 0);
                     }
-            };
-            if (group == 32)
-                chained(std::integral_constant<int, 1>{});
-            else if (group == 64)
-                chained(std::integral_constant<int, 2>{});
-            else
-                chained(std::integral_constant<int, 4>{});
+#pragma unroll
+                    for (int c = 0; c < kCT; ++c) {
+                        const float scale = scales.int4(c, d, t / kSame);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            sums.acc[m][c][0][r] = fmaf(scale, fmaf(-136.0f, sum[r], p[c][r]), sums.acc[m][c][0][r]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
         }
     }
 }
@@ -368,7 +374,7 @@ struct FewCursor {
     static constexpr int kRows = kTT ? kTT : 1, kActs = kTT ? Form::kChunks : 1;
     Panel panel[kCT];
     const unsigned char *act;
-    uint32_t act_bytes, act_tile, act_eights, act_magic; // eights: of columns in a tile; magic: 2^31 / eights, rounded up
+    uint32_t act_bytes, act_tile, act_wide; // wide: a tile has 16 columns (1) or 8 (0)
     uint32_t row_off[kRows];
     int line, end, groups; // next line, the segment's last, groups of kDepth lines left
 
@@ -385,8 +391,7 @@ struct FewCursor {
         act_bytes = a.bytes;
         if constexpr (kTiled) {
             act_tile = a.tile;
-            act_eights = (uint32_t)a.width / 8u;
-            act_magic = act_eights == 3 ? 0x2AAAAAABu : act_eights == 4 ? 0x20000000u : 0x80000000u >> (act_eights - 1);
+            act_wide = a.width == 16;
         }
 #pragma unroll
         for (int m = 0; m < kRows; ++m) {
@@ -399,8 +404,8 @@ struct FewCursor {
     {
         if constexpr (!kTiled)
             return (uint32_t)(col * Form::kElt);
-        const uint32_t n = (uint32_t)col / 8u, tile_at = __umulhi(2u * n, act_magic); // n / eights (n < 2^18)
-        return tile_at * act_tile + (n - tile_at * act_eights) * (8u * Form::kElt) + (uint32_t)(col % 8 * Form::kElt);
+        const uint32_t n = (uint32_t)col / 8u;
+        return (n >> act_wide) * act_tile + (n & act_wide) * (8u * Form::kElt) + (uint32_t)(col % 8 * Form::kElt);
     }
 };
 
@@ -437,7 +442,8 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
 #pragma unroll
         for (int t = 0; t < Ops::kActs; ++t) {
             const int col = c.line * Form::kLineCols + Cursor::chunk_col(kTT ? t : i % Form::kChunks);
-            const uint32_t at = !Form::kRagged || col < g.cols ? c.col_off(col) : kNowhere; // (past the row's end would be another row's)
+            // (past the row's end would be another row's)
+            const uint32_t at = c.col_off(col) | (!Form::kRagged || col < g.cols ? 0u : kNowhere);
 #pragma unroll
             for (int m = 0; m < Ops::kRows; ++m)
                 o.a[m][t] = __builtin_amdgcn_raw_buffer_load_b128(ra, (int)(at + c.row_off[m]), 0, 0);
@@ -449,8 +455,8 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
     // the scales of a group of lines, asked for before its first line
     auto fetch_scales = [&]() {
         if constexpr (Form::kQ4) {
-            constexpr int kBytes = kForm == kFewFp4 ? 1 : 2, kLoad = 4 * kBytes;
-            const int per_line = kForm == kFewFp4 || g.group == 32 ? 4 : g.group == 64 ? 2 : 1;
+            constexpr int kBytes = kForm == kFewFp4 ? 1 : 2, kLoad = 4 * FewScales<kForm, kCT>::kRegs;
+            constexpr int per_line = 4 / Form::kSame;
 #pragma unroll
             for (int f = 0; f < kFours; ++f)
 #pragma unroll
@@ -459,7 +465,7 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
                     const uint32_t want = (uint32_t)(i * g.scale_cols + (c.line + 4 * f + q) * per_line) * kBytes;
                     const uint32_t last = c.panel[p].scale_bytes - kLoad, at = want < last ? want : last;
                     scales[f].shift[p] = want - at < kLoad ? 8 * (want - at) : 0; // (further: of a row or line that is not there)
-                    if constexpr (kForm == kFewFp4) {
+                    if constexpr (kLoad == 4) {
                         scales[f].raw[p][0] = __builtin_amdgcn_raw_buffer_load_b32(rs, (int)at, 0, 0);
                     } else {
                         const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(rs, (int)at, 0, 0);
@@ -477,6 +483,7 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
         fetch(o[d]);
     FewSums<kForm, kTT, kCT> sums;
     sums.clear();
+    to_operand_lanes(o[0]);
     for (;;) {
         if (--c.groups == 0) { // the next group is another segment's
             if (source.open(c)) {
@@ -495,9 +502,16 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
         fetch_scales();
 #pragma unroll
         for (int d = 0; d < kDepth; ++d) {
-            few_multiply(sums, o[d], scales[Form::kQ4 ? d / 4 : 0], d % 4, g.group);
+            // (a line changes lanes under the products of the one before; a single line's ring has no such line)
+            if constexpr (kDepth > 1) {
+                to_operand_lanes(o[(d + 1) % kDepth]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            few_multiply(sums, o[d], scales[Form::kQ4 ? d / 4 : 0], d % 4);
             __builtin_amdgcn_sched_barrier(0);
             fetch(o[d]);
+            if constexpr (kDepth == 1)
+                to_operand_lanes(o[0]);
         }
         if (--left == 0) {
             source.close(sums);
@@ -509,6 +523,15 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
     }
 }
 
+// Lines in flight per wavefront: what 256 registers hold beside a line's products (registers of a line in the comment).
+template <int kForm, int kTT, int kCT>
+constexpr int few_depth()
+{
+    if (FewForm<kForm>::kQ4) // 4 kCT + 4, 16, 32
+        return kTT == 0 ? (FewForm<kForm>::kInt4 && kCT == 2 ? 4 : 8) : kTT == 1 ? 4 : 2;
+    return kTT <= 1 ? (kCT == 1 ? 8 : 4) : kCT == 1 ? 4 : 3; // 8 kCT + 4, 8, 16
+}
+
 // LDS and register barrier without the memory fence of __syncthreads, which would wait for the loads in flight.
 __device__ __forceinline__ void few_barrier()
 {
@@ -516,6 +539,88 @@ __device__ __forceinline__ void few_barrier()
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
+
+// The wavefronts of a workgroup draw units: items, or one of `parts` parts of an item's reduction.
+
+// The next number of a counter in LDS, for the wavefront.
+__device__ __forceinline__ int few_draw(int *counter)
+{
+    int n = 0;
+    if (threadIdx.x % kWave == 0)
+        n = atomicAdd(counter, 1);
+    return __builtin_amdgcn_readfirstlane(n);
+}
+
+// Parts (1, 2, 4 or 8) with which a workgroup's wavefronts are soonest through `items` items of `lines` lines each: a unit
+// takes whole groups of `depth` lines, and some time of its own; parts also meet in LDS.
+__device__ __forceinline__ int few_parts(int items, int lines, int depth)
+{
+    int best = 1, least = 0x7FFFFFFF;
+    for (int parts = 1; parts <= kFewWaves && (parts == 1 || parts <= lines); parts *= 2) {
+        const int turns = (items * parts + kFewWaves - 1) / kFewWaves, length = (lines + parts - 1) / parts;
+        const int time = turns * ((length + depth - 1) / depth * depth + (parts > 1 ? 3 : 2));
+        if (time < least)
+            least = time, best = parts;
+    }
+    return best;
+}
+
+// Room in LDS for items whose parts are under way: how far wavefronts may be apart.
+struct FewRoom {
+    int parts_done[8]; // of the item in a place
+    int item[8];       // that may use a place
+};
+
+// Where the parts of items 0, 1, .. of a workgroup meet.  A place in the pool is [part][tile][value][lane].
+template <int kForm, int kTT, int kCT>
+struct FewJoin {
+    static constexpr int kValues = kFewValues<kForm, kTT>, kPartFloats = kCT * kValues * kWave;
+    float *pool;
+    FewRoom &room;
+    int parts, places;
+
+    __device__ FewJoin(float *pool, int pool_floats, FewRoom &room, int parts) : pool(pool), room(room), parts(parts)
+    {
+        places = pool_floats / (parts * kPartFloats);
+        places = places < 8 ? places : 8;
+    }
+    // Part `part` of item n; whoever brings the last one calls done(total) with total(tile, value), added up in the parts'
+    // order.  A part waits until the item that had its place before is done with.  The oldest item that is not done never
+    // waits, and every wavefront closes its units in the order of their items: so every wait ends.
+    template <class Done>
+    __device__ __forceinline__ void close(const FewSums<kForm, kTT, kCT> &sums, int n, int part, Done done)
+    {
+        const int lane = threadIdx.x % kWave, place = n % places;
+        while (__builtin_amdgcn_readfirstlane(__hip_atomic_load(&room.item[place], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP)) != n)
+            __builtin_amdgcn_s_sleep(1);
+        float *const slot = pool + place * parts * kPartFloats;
+#pragma unroll
+        for (int c = 0; c < kCT; ++c)
+#pragma unroll
+            for (int v = 0; v < kValues; ++v)
+                slot[part * kPartFloats + (c * kValues + v) * kWave + lane] = sums.value(c, v);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // (LDS of a workgroup keeps its order)
+        if (few_draw(&room.parts_done[place]) != parts - 1)
+            return;
+        asm volatile("" ::: "memory");
+        done([&](int c, int v) {
+            float p[kFewWaves];
+#pragma unroll
+            for (int w = 0; w < kFewWaves; ++w) // (past the last part: the first, for nothing)
+                p[w] = slot[(w < parts ? w : 0) * kPartFloats + (c * kValues + v) * kWave + lane];
+            float all = p[0];
+#pragma unroll
+            for (int w = 1; w < kFewWaves; ++w)
+                all += w < parts ? p[w] : 0.0f;
+            return all;
+        });
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (lane == 0) {
+            room.parts_done[place] = 0;
+            __hip_atomic_store(&room.item[place], n + places, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        }
+    }
+};
 #endif
 
 }  // namespace moe
