@@ -13,10 +13,13 @@ namespace moe {
 // A workgroup has sixteen experts and the eight partials l = j, j + 8, ... (wavefront 0: the first four), which rounds 32,
 // 16 and 8 make one; the reader does rounds 4, 2, 1.  So even one token's router runs on E / 2 workgroups, and an XCD
 // (j = blockIdx.x % 8) has rows of W_r of its own.  Latency bound: all loads of 64 steps are in flight at once.
+// Further workgroups write x as the products with 4-bit weights want it (few_stream.h): a line's sixteens of eight columns
+// in the order of FewForm::kOwn (`own`), the columns of eight in int4_order (`order`), zeros past H.
 // ------------------------------------------------------------------------
 template <bool kBf16>
 __global__ __launch_bounds__(2 * kWave) void few_logits(const void *__restrict__ x, int N, int H, const float *__restrict__ W_r,
-                                                        int E, float *__restrict__ parts, uint32_t *flags, int flag_count)
+                                                        int E, float *__restrict__ parts, uint32_t *flags, int flag_count, u32x4 *packed, int own,
+                                                        int order)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int kBatch = 32;
@@ -24,6 +27,20 @@ __global__ __launch_bounds__(2 * kWave) void few_logits(const void *__restrict__
     const int lane = threadIdx.x % kWave, c = lane % 16, blk = lane / 16;
     const int half = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int j = (int)blockIdx.x % kParts, e0 = (int)blockIdx.x / kParts * 16, n0 = (int)blockIdx.y * 16;
+    const int logit_groups = (E + 15) / 16 * kParts;
+    if ((int)blockIdx.x >= logit_groups) {
+        if constexpr (kBf16) {
+            const int row = (H + 127) / 128 * 16, at = (((int)blockIdx.x - logit_groups) * (int)gridDim.y + (int)blockIdx.y) * (2 * kWave) + (int)threadIdx.x;
+            const int n = at / row, u = at % row;
+            if (n < N) {
+                u32x4 v = {0, 0, 0, 0};
+                if (8 * u < H)
+                    v = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(x) + (int64_t)n * H + 8 * u);
+                packed[n * row + (own ? u / 16 * 16 + u % 4 * 4 + u / 4 % 4 : u)] = order ? __builtin_bit_cast(u32x4, int4_order(v)) : v;
+            }
+        }
+        return;
+    }
     if (blockIdx.x == 0 && blockIdx.y == 0)
         for (int f = threadIdx.x; f < flag_count; f += 2 * kWave)
             flags[f] = 0;
@@ -92,25 +109,27 @@ __global__ __launch_bounds__(2 * kWave) void few_logits(const void *__restrict__
 struct FewWorkspace {
     uint32_t *flags;
     float *parts;
+    void *x; // packed
     void *a;
     size_t bytes;
 };
 
-static FewWorkspace few_carve(void *ws, int64_t N, int E, int K, int64_t F, int dtype)
+static FewWorkspace few_carve(void *ws, int64_t N, int64_t H, int E, int K, int64_t F, int dtype)
 {
     unsigned char *const w = static_cast<unsigned char *>(ws);
     const size_t elt = dtype == MOE_BF16 ? 2 : 4;
-    const size_t parts = kFlags * sizeof(uint32_t), a = parts + ((size_t)N * kParts * E * sizeof(float) + 127) / 128 * 128;
-    // tiles of at least 8 columns, each expert's in whole cache lines: at most 15 bytes a column are lost
-    const size_t rows = (size_t)N * K, experts = rows < (size_t)E ? rows : (size_t)E, cols = F + 32;
-    return {reinterpret_cast<uint32_t *>(w), reinterpret_cast<float *>(w + parts), w + a,
+    const size_t parts = kFlags * sizeof(uint32_t), x = parts + ((size_t)N * kParts * E * sizeof(float) + 127) / 128 * 128;
+    const size_t a = x + (dtype == MOE_BF16 ? (size_t)N * ((H + 127) / 128) * 256 : 0);
+    // tiles of at least 8 columns, each expert's (an expert may have two entries) in whole cache lines: at most 15 bytes a
+    // column are lost
+    const size_t rows = (size_t)N * K, experts = (rows < (size_t)E ? rows : (size_t)E) + rows / (kFewMost + 1), cols = F + 32;
+    return {reinterpret_cast<uint32_t *>(w), reinterpret_cast<float *>(w + parts), w + x, w + a,
             a + rows * cols * elt + experts * cols * 16};
 }
 
 size_t few_workspace_bytes(int64_t N, int64_t H, int E, int K, int64_t F, int dtype)
 {
-    (void)H;
-    return few_carve(nullptr, N, E, K, F, dtype).bytes;
+    return few_carve(nullptr, N, H, E, K, F, dtype).bytes;
 }
 
 // Width of the gate/up items and parts of their reduction: the least time of the longest share, in units of a line of one
@@ -132,7 +151,7 @@ static void choose_items(FewKernelArgs &g, double experts)
 
 int launch_layer_few(const FewArgs &args, int dtype, int format, hipStream_t st)
 {
-    const FewWorkspace w = few_carve(args.ws, args.N, args.E, args.K, args.F, dtype);
+    const FewWorkspace w = few_carve(args.ws, args.N, args.H, args.E, args.K, args.F, dtype);
     const int cus = compute_units();
     FewKernelArgs g = {};
     g.l = args;
@@ -159,11 +178,18 @@ int launch_layer_few(const FewArgs &args, int dtype, int format, hipStream_t st)
         g.down_parts *= 2;
     const char *const patience = getenv("MOE_FEW_PATIENCE"); // (tests: 0 makes every workgroup take over what is missing)
     g.patience = patience ? atoi(patience) : kDefaultPatience;
-    const dim3 grid((unsigned)(ceil_div(args.E, 16) * kParts), (unsigned)ceil_div(args.N, 16));
+    const bool packed = format != kNoFormat;
+    g.x = packed ? w.x : args.x;
+    g.x_cols = packed ? g.h_lines * 128 : args.H;
+    const int64_t rows16 = ceil_div(args.N, 16), copies = packed ? ceil_div((int64_t)args.N * g.h_lines * 16, 2 * kWave * rows16) : 0;
+    const dim3 grid((unsigned)(ceil_div(args.E, 16) * kParts + copies), (unsigned)rows16);
+    const int own = format == MOE_Q4_FP4 || args.group == 128, order = format == MOE_Q4_INT4;
     if (dtype == MOE_BF16)
-        hipLaunchKernelGGL(few_logits<true>, grid, dim3(2 * kWave), 0, st, args.x, args.N, args.H, args.W_r, args.E, w.parts, w.flags, kFlags);
+        hipLaunchKernelGGL(few_logits<true>, grid, dim3(2 * kWave), 0, st, args.x, args.N, args.H, args.W_r, args.E, w.parts, w.flags, kFlags,
+                           static_cast<u32x4 *>(w.x), own, order);
     else
-        hipLaunchKernelGGL(few_logits<false>, grid, dim3(2 * kWave), 0, st, args.x, args.N, args.H, args.W_r, args.E, w.parts, w.flags, kFlags);
+        hipLaunchKernelGGL(few_logits<false>, grid, dim3(2 * kWave), 0, st, args.x, args.N, args.H, args.W_r, args.E, w.parts, w.flags, kFlags,
+                           static_cast<u32x4 *>(w.x), own, order);
     if (format == MOE_Q4_FP4)
         launch_few_ffn<kFewFp4>(g, st);
     else if (format == MOE_Q4_INT4 && args.group == 32)

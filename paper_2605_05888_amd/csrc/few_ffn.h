@@ -46,6 +46,8 @@ constexpr int kDefaultPatience = 1 << 15; // polls (about a microsecond each): l
 struct FewKernelArgs {
     FewArgs l;
     const float *parts;
+    const void *x; // as gate/up reads it: packed for 4-bit weights
+    int x_cols;    // of a row of it
     uint32_t *flags;
     int shares;    // of gate/up items
     int width;      // columns of F of an item: 8 or 16
@@ -245,7 +247,7 @@ template <int kForm, int kTT>
 struct GateUp {
     using Form = FewForm<kForm>;
     static constexpr int kCT = 2, kDepth = few_depth<kForm, kTT, kCT>(); // tiles: gate, up
-    static constexpr int kValues = kFewValues<kForm, kTT>;
+    static constexpr int kValues = kFewValues<kForm, kTT>, kActs = Form::kQ4 ? kActPacked : kActRows;
     const FewKernelArgs &g;
     const FewArgs &l;
     const FewLists &lists;
@@ -271,7 +273,7 @@ struct GateUp {
         before += items;
         parts = __builtin_amdgcn_readfirstlane(few_parts(mine, g.h_lines, kDepth));
     }
-    __device__ __forceinline__ bool open(FewCursor<kForm, kTT, kCT, false> &c)
+    __device__ __forceinline__ bool open(FewCursor<kForm, kTT, kCT, kActs> &c)
     {
         const int u = few_draw(counter);
         if (u >= mine * parts)
@@ -286,8 +288,8 @@ struct GateUp {
         const int64_t row = (int64_t)expert * l.F + f0, end = row + (l.F - f0 < g.width ? l.F - f0 : g.width);
         c.panel[0] = panel_of<kForm>(l.gate, row, end, l.H, l.scale_cols_h);
         c.panel[1] = panel_of<kForm>(l.up, row, end, l.H, l.scale_cols_h);
-        const uint32_t x_row = (uint32_t)l.H * Form::kElt;
-        c.set_acts({static_cast<const unsigned char *>(l.x), (uint32_t)l.N * x_row, 0, 0, rows},
+        const uint32_t x_row = (uint32_t)g.x_cols * Form::kElt;
+        c.set_acts({static_cast<const unsigned char *>(g.x), (uint32_t)l.N * x_row, 0, 0, rows},
                    [&](int r) { return lists.token[base + r] * x_row; });
         c.line = g.h_lines * open_unit.part / parts;
         c.end = g.h_lines * (open_unit.part + 1) / parts;
@@ -302,14 +304,17 @@ struct GateUp {
         const FewActs to = few_activation<kForm>(g, lists, unit.at, rows);
         const int r = few_row_of<kForm, kTT>(v), i = threadIdx.x % 16;
         const bool there = r < rows && i < g.width && unit.tile * g.width + i < l.F;
-        unsigned char *const put = const_cast<unsigned char *>(to.data) + (int64_t)unit.tile * to.tile + (r * g.width + i) * Form::kElt;
+        const int col = i % 8;
+        unsigned char *const put = const_cast<unsigned char *>(to.data) + (int64_t)unit.tile * to.tile + (i / 8 * rows + r) * (8 * Form::kElt);
         if constexpr (kForm == kFewF32) {
             if (there)
-                __hip_atomic_store(reinterpret_cast<uint32_t *>(put), __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        } else { // the even lane stores both columns (F and width are even)
-            const uint32_t both = pack_bf16x2(a, __shfl_xor(a, 1));
-            if (there && threadIdx.x % 2 == 0)
-                __hip_atomic_store(reinterpret_cast<uint32_t *>(put), both, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __hip_atomic_store(reinterpret_cast<uint32_t *>(put) + col, __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        } else { // one lane stores two columns (F and width are even): neighbours, or (INT4) those that int4_order has side by side
+            constexpr int kOther = Form::kInt4 ? 2 : 1;
+            const int place = Form::kInt4 ? col / 4 + col % 2 * 2 : col / 2;
+            const uint32_t both = pack_bf16x2(a, __shfl_xor(a, kOther));
+            if (there && (threadIdx.x & kOther) == 0)
+                __hip_atomic_store(reinterpret_cast<uint32_t *>(put) + place, both, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
     }
     __device__ __forceinline__ void close(const FewSums<kForm, kTT, kCT> &sums)
@@ -352,7 +357,7 @@ struct Down {
         begin = __builtin_amdgcn_readfirstlane(lists.begin[cls]);
         units = (__builtin_amdgcn_readfirstlane(lists.begin[cls + 1]) - begin) * g.down_parts;
     }
-    __device__ __forceinline__ bool open(FewCursor<kForm, kTT, kCT, true> &c)
+    __device__ __forceinline__ bool open(FewCursor<kForm, kTT, kCT, kActTiles> &c)
     {
         const int u = few_draw(counter);
         if (u >= units)
@@ -367,8 +372,7 @@ struct Down {
 #pragma unroll
         for (int p = 0; p < kCT; ++p)
             c.panel[p] = panel_of<kForm>(l.down, row + 16 * p, end, l.F, l.scale_cols_f);
-        const uint32_t a_row = (uint32_t)g.width * Form::kElt;
-        c.set_acts(few_activation<kForm>(g, lists, at, rows), [&](int r) { return r * a_row; });
+        c.set_acts(few_activation<kForm>(g, lists, at, rows), [](int r) { return r * (8u * Form::kElt); });
         c.line = g.f_lines * open_unit.part / g.down_parts;
         c.end = g.f_lines * (open_unit.part + 1) / g.down_parts;
         c.groups = c.end > c.line ? (c.end - c.line + kDepth - 1) / kDepth : 1;
@@ -467,7 +471,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
                 return;
             using Items = GateUp<kForm, kTT>;
             Items items(g, lists, sh.pool, room, counters + cls, cls, who, before);
-            few_stream<kForm, kTT, Items::kCT, Items::kDepth, false>(items, in);
+            few_stream<kForm, kTT, Items::kCT, Items::kDepth, Items::kActs>(items, in);
             if (items.parts > 1) { // (the next class has other places in the pool)
                 few_barrier();
                 restart();
@@ -494,7 +498,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
                 return;
             using Part = Down<kForm, kTT, kCT>;
             Part part(g, lists, sh.pool, counters + cls, cls, h0, cols);
-            few_stream<kForm, kTT, kCT, Part::kDepth, true>(part, mid);
+            few_stream<kForm, kTT, kCT, Part::kDepth, kActTiles>(part, mid);
         };
         down(std::integral_constant<int, 0>{}, 0);
         down(std::integral_constant<int, 1>{}, 1);

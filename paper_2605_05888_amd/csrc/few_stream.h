@@ -52,11 +52,15 @@ struct FewForm {
     static constexpr int kChunks = kQ4 ? 4 : 2;
     static constexpr int kFewRows = 16 / kChunks;
     static constexpr bool kRagged = kForm != kFewBf16;                           // the last line may be cut short
+    static constexpr bool kOwn = kForm == kFewFp4 || kForm == kFewInt4By128;     // packed: a lane's columns of a line are its own
     __host__ __device__ static constexpr int64_t row_bytes(int64_t cols) { return kQ4 ? cols / 2 : cols * kElt; }
 };
 
 constexpr int kFewWaves = 8, kFewThreads = kFewWaves * kWave; // of a workgroup
 constexpr int kFewMost = 32; // rows of a stream: what 256 registers hold
+// How the activations of a stream are laid out: rows as the caller has them; rows, or tiles, as the operands want them.
+enum { kActRows, kActPacked, kActTiles };
+
 constexpr uint32_t kNowhere = 0x40000000u; // an offset past every byte count used here, twice too: loads give zeros
 
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -96,8 +100,8 @@ __device__ __forceinline__ Panel panel_of(const FewMatrix &w, int64_t row, int64
     return p;
 }
 
-// Where the activations of a segment are, all below `bytes`.  Row-major (width 0): rows at row_of(r).  Else tiles of `width`
-// columns (8 or 16), `tile` bytes apart, and in a tile the rows at row_of(r).
+// Where the activations of a segment are, all below `bytes`: rows at row_of(r), or tiles of `width` columns (8 or 16), `tile`
+// bytes apart: in a tile eight columns of all rows, then the other eight.
 struct FewActs {
     const unsigned char *data;
     uint32_t bytes;
@@ -208,9 +212,12 @@ struct FewScales {
     uint32_t shift[kCT]; // bits that a load was moved back by, so as not to pass the panel's end
     uint32_t of[kCT][4][kRegs];
 
+    // own: of an FP4 line a lane needs the scale of its own group only
+    template <bool kOwn>
     __device__ __forceinline__ void spread()
     {
         const int row = (int)(threadIdx.x % 16) * 16; // byte address of the lane that fetched line 0's of row i
+        const int mine = (int)(threadIdx.x % kWave / 16) * 8;
 #pragma unroll
         for (int c = 0; c < kCT; ++c) {
             if constexpr (kRegs == 2) {
@@ -222,12 +229,20 @@ struct FewScales {
 #pragma unroll
             for (int r = 0; r < kRegs; ++r)
 #pragma unroll
-                for (int d = 0; d < 4; ++d)
-                    of[c][d][r] = (uint32_t)__builtin_amdgcn_ds_bpermute(row + 4 * d, (int)raw[c][r]);
+                for (int d = 0; d < 4; ++d) {
+                    uint32_t v = (uint32_t)__builtin_amdgcn_ds_bpermute(row + 4 * d, (int)raw[c][r]);
+                    if constexpr (kOwn && kForm == kFewFp4)
+                        v = v >> mine & 0xFFu;
+                    of[c][d][r] = v;
+                }
         }
     }
-    // of group t of 32 columns in line d (0 .. 3)
-    __device__ __forceinline__ float fp4(int c, int d, int t) const { return fp4_scale(of[c][d][0] >> (8 * t) & 0xFFu); }
+    // of the columns of instruction t in line d (0 .. 3)
+    template <bool kOwn>
+    __device__ __forceinline__ float fp4(int c, int d, int t) const
+    {
+        return fp4_scale(kOwn ? of[c][d][0] : of[c][d][0] >> (8 * t) & 0xFFu);
+    }
     __device__ __forceinline__ float int4(int c, int d, int place) const
     {
         const uint32_t v = of[c][d][kRegs == 2 ? place / 2 : 0];
@@ -236,36 +251,44 @@ struct FewScales {
 };
 
 // What a lane has fetched, to the lane whose operand it is.
-__device__ __forceinline__ void to_operand_lane(u32x4 &v)
+__device__ __forceinline__ void from_lane(u32x4 &v, int from)
 {
-    const int from = (int)(threadIdx.x % 16 * 4 + threadIdx.x % kWave / 16) * 4;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        v[j] = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)v[j]);
+        v[j] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * from, (int)v[j]);
 }
 
-template <int kForm, int kTT, int kCT>
+template <int kForm, int kTT, int kCT, int kActs>
 __device__ __forceinline__ void to_operand_lanes(FewOperands<kForm, kTT, kCT> &o)
 {
+    using Form = FewForm<kForm>;
+    const int i = (int)(threadIdx.x % 16), q = (int)(threadIdx.x % kWave / 16);
 #pragma unroll
     for (int c = 0; c < kCT; ++c)
 #pragma unroll
-        for (int l = 0; l < FewForm<kForm>::kLoads; ++l)
-            to_operand_lane(o.w[c][l]);
+        for (int l = 0; l < Form::kLoads; ++l)
+            from_lane(o.w[c][l], 4 * i + q);
+    if constexpr (kActs != kActTiles) {
 #pragma unroll
-    for (int m = 0; m < FewOperands<kForm, kTT, kCT>::kRows; ++m)
+        for (int m = 0; m < FewOperands<kForm, kTT, kCT>::kRows; ++m)
 #pragma unroll
-        for (int t = 0; t < FewOperands<kForm, kTT, kCT>::kActs; ++t)
-            to_operand_lane(o.a[m][t]);
+            for (int t = 0; t < FewOperands<kForm, kTT, kCT>::kActs; ++t)
+                from_lane(o.a[m][t], 4 * i + q);
+    } else if constexpr (kTT == 0) {
+        const int t = i % Form::kChunks, piece = Form::kOwn ? Form::kChunks * q + t : 4 * t + q;
+        from_lane(o.a[0][0], piece * Form::kFewRows + i / Form::kChunks);
+    }
 }
 
 // Line d of four.
-template <int kForm, int kTT, int kCT>
+template <int kForm, int kTT, int kCT, int kActs>
 __device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, const FewOperands<kForm, kTT, kCT> &o,
                                              const FewScales<kForm, kCT> &scales, int d)
 {
     using Form = FewForm<kForm>;
     using Ops = FewOperands<kForm, kTT, kCT>;
+    constexpr bool kPacked = kActs != kActRows, kOwn = kPacked && Form::kOwn;
+    auto words = [&](int c) { return kOwn ? o.w[c][0] : transpose_quads(o.w[c][0]); }; // of the instructions
     const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
     if constexpr (kForm == kFewF32) {
 #pragma unroll
@@ -285,14 +308,14 @@ __device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, con
         if constexpr (kForm == kFewFp4)
 #pragma unroll
             for (int c = 0; c < kCT; ++c)
-                codes[c] = transpose_quads(o.w[c][0]);
+                codes[c] = words(c);
 #pragma unroll
         for (int t = 0; t < Form::kChunks; ++t)
 #pragma unroll
             for (int c = 0; c < kCT; ++c) {
                 bf16x8 w;
                 if constexpr (kForm == kFewFp4)
-                    w = fp4_operand(codes[c][t], scales.fp4(c, d, t));
+                    w = fp4_operand(codes[c][t], scales.template fp4<kOwn>(c, d, t));
                 else
                     w = __builtin_bit_cast(bf16x8, o.w[c][t]);
 #pragma unroll
@@ -302,20 +325,20 @@ __device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, con
                 }
             }
     } else {
+        // -136 times the activations' sum is where an instruction starts from
         constexpr int kSame = Form::kSame;
-        const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
+        const bf16x8 minus = __builtin_bit_cast(bf16x8, u32x4{0xC308C308u, 0xC308C308u, 0xC308C308u, 0xC308C308u});
+        auto act = [&](const u32x4 &a) { return kPacked ? __builtin_bit_cast(bf16x8, a) : int4_order(a); };
         if constexpr (kTT == 0) {
-            const bf16x8 a = int4_order(o.a[0][0]);
-            const f32x4 sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, ones, zero, 0, 0, 0);
+            const bf16x8 a = act(o.a[0][0]);
+            const f32x4 sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, minus, zero, 0, 0, 0);
 #pragma unroll
             for (int c = 0; c < kCT; ++c) {
-                const u32x4 codes = transpose_quads(o.w[c][0]);
+                const u32x4 codes = words(c);
                 float v[4];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const f32x4 p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, int4_operand(codes[t]), zero, 0, 0, 0);
-                    v[t] = fmaf(-136.0f, sum[t], p[t]);
-                }
+                for (int t = 0; t < 4; ++t)
+                    v[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, int4_operand(codes[t]), sum, 0, 0, 0)[t];
 #pragma unroll
                 for (int t = 0; t < 4; t += kSame) {
                     float all = v[t];
@@ -330,7 +353,7 @@ __device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, con
             u32x4 codes[kCT];
 #pragma unroll
             for (int c = 0; c < kCT; ++c)
-                codes[c] = transpose_quads(o.w[c][0]);
+                codes[c] = words(c);
 #pragma unroll
             for (int t = 0; t < 4; t += kSame) {
                 bf16x8 w[kCT][kSame];
@@ -343,22 +366,22 @@ __device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, con
                 for (int m = 0; m < Ops::kRows; ++m) {
                     f32x4 sum = zero, p[kCT];
 #pragma unroll
-                    for (int c = 0; c < kCT; ++c)
-                        p[c] = zero;
+                    for (int u = 0; u < kSame; ++u)
+                        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(act(o.a[m][t + u]), minus, sum, 0, 0, 0);
 #pragma unroll
-                    for (int u = 0; u < kSame; ++u) {
-                        const bf16x8 a = int4_order(o.a[m][kTT ? t + u : 0]);
-                        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, ones, sum, 0, 0, 0);
+                    for (int c = 0; c < kCT; ++c)
+                        p[c] = sum;
+#pragma unroll
+                    for (int u = 0; u < kSame; ++u)
 #pragma unroll
                         for (int c = 0; c < kCT; ++c)
-                            p[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[c][u], p[c], 0, 0, 0);
-                    }
+                            p[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(act(o.a[m][t + u]), w[c][u], p[c], 0, 0, 0);
 #pragma unroll
                     for (int c = 0; c < kCT; ++c) {
                         const float scale = scales.int4(c, d, t / kSame);
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            sums.acc[m][c][0][r] = fmaf(scale, fmaf(-136.0f, sum[r], p[c][r]), sums.acc[m][c][0][r]);
+                            sums.acc[m][c][0][r] = fmaf(scale, p[c][r], sums.acc[m][c][0][r]);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -368,44 +391,56 @@ __device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, con
 }
 
 // Where the stream's next lines are fetched from: panels and activations of one segment, for this lane.
-template <int kForm, int kTT, int kCT, bool kTiled>
+template <int kForm, int kTT, int kCT, int kActs>
 struct FewCursor {
     using Form = FewForm<kForm>;
-    static constexpr int kRows = kTT ? kTT : 1, kActs = kTT ? Form::kChunks : 1;
+    static constexpr int kRows = kTT ? kTT : 1;
+    static constexpr int kPiece = 16 / Form::kElt; // columns of a load
     Panel panel[kCT];
     const unsigned char *act;
-    uint32_t act_bytes, act_tile, act_wide; // wide: a tile has 16 columns (1) or 8 (0)
+    uint32_t act_bytes, act_tile, act_eight, act_wide; // eight: bytes of eight columns; wide: a tile has 16 columns (1) or 8 (0)
     uint32_t row_off[kRows];
     int line, end, groups; // next line, the segment's last, groups of kDepth lines left
 
-    // first column of chunk t that this lane fetches
-    static __device__ __forceinline__ int chunk_col(int t)
+    // Row r of sixteens m of the activations that this lane fetches, and the first column in the line of its load t.  Rows:
+    // four neighbours 64 bytes of one.  Tiles: as many neighbours as there are rows the same columns.
+    static __device__ __forceinline__ int lane_row(int m)
     {
-        return (Form::kLineCols / Form::kChunks) * t + (16 / Form::kElt) * (int)(threadIdx.x % 4);
+        const int lane = threadIdx.x % kWave;
+        if constexpr (kActs == kActTiles)
+            return kTT ? 16 * m + lane % 16 : lane % Form::kFewRows;
+        return kTT ? 16 * m + lane / 4 : lane / 4 / Form::kChunks;
+    }
+    static __device__ __forceinline__ int lane_col(int t)
+    {
+        const int lane = threadIdx.x % kWave;
+        if constexpr (kActs == kActTiles)
+            return kPiece * (kTT == 0 ? lane / Form::kFewRows : Form::kOwn ? Form::kChunks * (lane / 16) + t : 4 * t + lane / 16);
+        return Form::kLineCols / Form::kChunks * (kTT ? t : lane / 4 % Form::kChunks) + kPiece * (lane % 4);
     }
     template <class RowOf>
     __device__ __forceinline__ void set_acts(const FewActs &a, RowOf row_of)
     {
-        const int i = threadIdx.x % kWave / 4;
         act = a.data;
         act_bytes = a.bytes;
-        if constexpr (kTiled) {
+        if constexpr (kActs == kActTiles) {
             act_tile = a.tile;
+            act_eight = (uint32_t)a.rows * (8u * Form::kElt);
             act_wide = a.width == 16;
         }
 #pragma unroll
         for (int m = 0; m < kRows; ++m) {
-            const int r = kTT ? 16 * m + i : i / Form::kChunks;
+            const int r = lane_row(m);
             row_off[m] = r < a.rows ? row_of(r) : kNowhere;
         }
     }
     // Byte offset of a column in its row.
     __device__ __forceinline__ uint32_t col_off(int col) const
     {
-        if constexpr (!kTiled)
+        if constexpr (kActs != kActTiles)
             return (uint32_t)(col * Form::kElt);
         const uint32_t n = (uint32_t)col / 8u;
-        return (n >> act_wide) * act_tile + (n & act_wide) * (8u * Form::kElt) + (uint32_t)(col % 8 * Form::kElt);
+        return (n >> act_wide) * act_tile + (n & act_wide) * act_eight + (uint32_t)(col % 8 * Form::kElt);
     }
 };
 
@@ -416,12 +451,12 @@ struct FewCursor {
 //   close(sums)     takes the sums of the oldest open segment
 // A group is written out straight, so that what is waited for is the same on every path: segments change between groups only.
 // (With a change possible at every line the code is kDepth times as long, 180 KB, and waits for nearly everything in flight.)
-template <int kForm, int kTT, int kCT, int kDepth, bool kTiled, class Source>
+template <int kForm, int kTT, int kCT, int kDepth, int kActs, class Source>
 __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
 {
     using Form = FewForm<kForm>;
     using Ops = FewOperands<kForm, kTT, kCT>;
-    using Cursor = FewCursor<kForm, kTT, kCT, kTiled>;
+    using Cursor = FewCursor<kForm, kTT, kCT, kActs>;
     Cursor c;
     if (!source.open(c))
         return;
@@ -441,9 +476,9 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
         const auto ra = few_buffer(c.act, there ? c.act_bytes : 0u);
 #pragma unroll
         for (int t = 0; t < Ops::kActs; ++t) {
-            const int col = c.line * Form::kLineCols + Cursor::chunk_col(kTT ? t : i % Form::kChunks);
+            const int col = c.line * Form::kLineCols + Cursor::lane_col(t);
             // (past the row's end would be another row's)
-            const uint32_t at = c.col_off(col) | (!Form::kRagged || col < g.cols ? 0u : kNowhere);
+            const uint32_t at = c.col_off(col) | (!Form::kRagged || kActs == kActPacked || col < g.cols ? 0u : kNowhere);
 #pragma unroll
             for (int m = 0; m < Ops::kRows; ++m)
                 o.a[m][t] = __builtin_amdgcn_raw_buffer_load_b128(ra, (int)(at + c.row_off[m]), 0, 0);
@@ -483,7 +518,7 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
         fetch(o[d]);
     FewSums<kForm, kTT, kCT> sums;
     sums.clear();
-    to_operand_lanes(o[0]);
+    to_operand_lanes<kForm, kTT, kCT, kActs>(o[0]);
     for (;;) {
         if (--c.groups == 0) { // the next group is another segment's
             if (source.open(c)) {
@@ -496,7 +531,7 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
         if constexpr (Form::kQ4) {
 #pragma unroll
             for (int f = 0; f < kFours; ++f)
-                scales[f].spread();
+                scales[f].template spread<(kActs != kActRows && Form::kOwn)>();
             __builtin_amdgcn_sched_barrier(0);
         }
         fetch_scales();
@@ -504,14 +539,14 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
         for (int d = 0; d < kDepth; ++d) {
             // (a line changes lanes under the products of the one before; a single line's ring has no such line)
             if constexpr (kDepth > 1) {
-                to_operand_lanes(o[(d + 1) % kDepth]);
+                to_operand_lanes<kForm, kTT, kCT, kActs>(o[(d + 1) % kDepth]);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            few_multiply(sums, o[d], scales[Form::kQ4 ? d / 4 : 0], d % 4);
+            few_multiply<kForm, kTT, kCT, kActs>(sums, o[d], scales[Form::kQ4 ? d / 4 : 0], d % 4);
             __builtin_amdgcn_sched_barrier(0);
             fetch(o[d]);
             if constexpr (kDepth == 1)
-                to_operand_lanes(o[0]);
+                to_operand_lanes<kForm, kTT, kCT, kActs>(o[0]);
         }
         if (--left == 0) {
             source.close(sums);

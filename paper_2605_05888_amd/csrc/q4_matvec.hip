@@ -115,7 +115,7 @@ struct MatvecItems {
         lines = (g.cols + Form::kLineCols - 1) / Form::kLineCols;
         parts = __builtin_amdgcn_readfirstlane(few_parts(mine, lines, kDepth));
     }
-    __device__ __forceinline__ bool open(FewCursor<kForm, kTT, kCT, false> &c)
+    __device__ __forceinline__ bool open(FewCursor<kForm, kTT, kCT, kActRows> &c)
     {
         const int u = few_draw(counter);
         if (u >= mine * parts)
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void q4_matvec(MatvecArgs g, int E)
             }
             few_barrier();
             MatvecItems<kForm, kTT, kCT> part(g, lists, pool, room, &counter, e0, segments, panels, first, mine);
-            few_stream<kForm, kTT, kCT, part.kDepth, false>(part, cols);
+            few_stream<kForm, kTT, kCT, part.kDepth, kActRows>(part, cols);
         };
         run(std::integral_constant<int, 2>{}, 2);
         run(std::integral_constant<int, 1>{}, 1);
