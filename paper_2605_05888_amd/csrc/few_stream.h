@@ -210,6 +210,7 @@ struct FewScales {
     static constexpr int kRegs = kForm == kFewInt4By32 ? 2 : 1;
     uint32_t raw[kCT][kRegs];
     uint32_t shift[kCT]; // bits that a load was moved back by, so as not to pass the panel's end
+    uint32_t keep[kRegs]; // of the segment: past it may be another row's, an infinity or NaN, which times zero is not zero
     uint32_t of[kCT][4][kRegs];
 
     // own: of an FP4 line a lane needs the scale of its own group only
@@ -222,9 +223,9 @@ struct FewScales {
         for (int c = 0; c < kCT; ++c) {
             if constexpr (kRegs == 2) {
                 const uint64_t v = ((uint64_t)raw[c][1] << 32 | raw[c][0]) >> (shift[c] & 63);
-                raw[c][0] = (uint32_t)v, raw[c][1] = (uint32_t)(v >> 32);
+                raw[c][0] = (uint32_t)v & keep[0], raw[c][1] = (uint32_t)(v >> 32) & keep[1];
             } else {
-                raw[c][0] >>= shift[c];
+                raw[c][0] = raw[c][0] >> shift[c] & keep[0];
             }
 #pragma unroll
             for (int r = 0; r < kRegs; ++r)
@@ -470,8 +471,12 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
         for (int p = 0; p < kCT; ++p) {
             const auto rw = few_buffer(c.panel[p].data, there ? c.panel[p].bytes : 0u);
 #pragma unroll
-            for (int s = 0; s < Form::kLoads; ++s)
-                o.w[p][s] = __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(w_off + (uint32_t)(c.line * Form::kLineBytes + 64 * s)), 0, 0);
+            for (int s = 0; s < Form::kLoads; ++s) {
+                uint32_t at = w_off + (uint32_t)(c.line * Form::kLineBytes + 64 * s);
+                if constexpr (kForm == kFewF32) // (past the row's end: the next row's, whose infinities and NaN stay its own)
+                    at |= c.line * Form::kLineCols + 16 * s + 4 * q < g.cols ? 0u : kNowhere;
+                o.w[p][s] = __builtin_amdgcn_raw_buffer_load_b128(rw, (int)at, 0, 0);
+            }
         }
         const auto ra = few_buffer(c.act, there ? c.act_bytes : 0u);
 #pragma unroll
@@ -492,8 +497,16 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
         if constexpr (Form::kQ4) {
             constexpr int kBytes = kForm == kFewFp4 ? 1 : 2, kLoad = 4 * FewScales<kForm, kCT>::kRegs;
             constexpr int per_line = 4 / Form::kSame;
+            const int groups = g.scale_cols < c.end * per_line ? g.scale_cols : c.end * per_line;
 #pragma unroll
-            for (int f = 0; f < kFours; ++f)
+            for (int f = 0; f < kFours; ++f) {
+                const int left = groups - (c.line + 4 * f + q) * per_line;
+#pragma unroll
+                for (int r = 0; r < FewScales<kForm, kCT>::kRegs; ++r) {
+                    constexpr int per_reg = 4 / kBytes;
+                    const int n = left - per_reg * r;
+                    scales[f].keep[r] = n >= per_reg ? 0xFFFFFFFFu : n > 0 ? (1u << (8 * kBytes * n)) - 1 : 0u;
+                }
 #pragma unroll
                 for (int p = 0; p < kCT; ++p) {
                     const auto rs = few_buffer(c.panel[p].scales, c.line < c.end ? c.panel[p].scale_bytes : 0u);
@@ -507,6 +520,7 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
                         scales[f].raw[p][0] = v[0], scales[f].raw[p][1] = v[1];
                     }
                 }
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     };

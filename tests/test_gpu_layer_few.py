@@ -141,6 +141,36 @@ def test_masked_experts_beyond_the_picks_and_overflow_keep_the_picks_distinct():
 
 
 @pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("N,K", [(2, 1), (9, 4), (40, 3)])
+def test_what_is_not_finite_in_a_row_of_down_stays_in_its_column(form, N, K):
+    """Weights (4 bits: scales) of some rows are infinite, NaN or of the largest size: the other columns keep their bits, also
+    where a row ends inside a cache line and the next one begins there."""
+    import torch
+    H, F = (132, 100) if form == "f32" else (192, 320)
+    t = Layer(form, N, H, 6, K, F)
+    want = t.call().clone()
+    rows = [0, 5, 21, 64, 65, 101, H - 1]
+    bad = (0x7F80, 0x7FC0, 0xFF80, 0x7F7F)
+    codes = t.w[2][0] if isinstance(form, tuple) else t.w[2]
+    scales = t.w[2][1] if isinstance(form, tuple) else None
+    for j, r in enumerate(rows):
+        if form == "f32":
+            codes[:, r] = (np.inf, np.nan, -np.inf, 3.4e38)[j % 4]
+        elif form == "bf16":
+            codes[:, r] = bad[j % 4]
+        elif form[0] == ref.FP4:
+            codes[:, r], scales[:, r] = 0x77, 254
+        else:
+            scales[:, r] = bad[j % 4]
+    t.on_device()
+    got = t.call()
+    rest = [h for h in range(H) if h not in rows]
+    assert bool(torch.isfinite(got[:, rest].float()).all())
+    assert torch.equal(got[:, rest], want[:, rest])
+    assert not bool(torch.isfinite(got[:, rows[:3]].float()).any())
+
+
+@pytest.mark.parametrize("form", FORMS)
 def test_equal_calls_give_equal_bits_whatever_the_workspace_held(form):
     import torch
     t = Layer(form, 21, 512, 32, 4, 384, SOFT)

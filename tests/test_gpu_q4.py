@@ -157,6 +157,31 @@ def test_matvec(fmt, group, counts, M, cols, rows):
     assert (ref.f64(got[:lead]) == 7.0).all() and (ref.f64(got[M - behind:]) == 7.0).all()
 
 
+@pytest.mark.parametrize("fmt,group", FORMATS)
+@pytest.mark.parametrize("M", [1, 4, 11, 40])
+def test_matvec_with_scales_that_are_not_finite_keeps_its_other_columns(fmt, group, M):
+    import torch
+    import paper_2605_05888_amd as hub
+    rng = np.random.default_rng(M)
+    for cols in (64, 320):
+        codes, scales = random_q4(rng, (48, cols), fmt, group)
+        x = dev(mi.f32_to_bf16_bits(rng.standard_normal((M, cols)).astype(np.float32)))
+        y = [torch.zeros((M, 48), dtype=torch.bfloat16, device="cuda:0") for _ in range(2)]
+        hub.moe_matvec_q4(x, None, dev(codes[None]), dev(scales[None]), fmt, group, y[0])
+        rows = [0, 7, 16, 33, 47]
+        scales[rows] = 254 if fmt == ref.FP4 else 0x7F80
+        codes[rows] = 0x77
+        hub.moe_matvec_q4(x, None, dev(codes[None]), dev(scales[None]), fmt, group, y[1])
+        rest = [r for r in range(48) if r not in rows]
+        assert bool(torch.isfinite(y[1][:, rest].float()).all())
+        assert torch.equal(y[0][:, rest], y[1][:, rest])
+
+
+@pytest.mark.parametrize("counts,M,cols,rows", [(sorted([0] * 900 + [1, 3, 20, 40] * 45, key=lambda c: c * 7919 % 13), 0, 64, 24), ([0] * 1500 + [2], 0, 128, 8)])
+def test_matvec_of_more_matrices_than_have_lists_at_a_time(counts, M, cols, rows):
+    test_matvec(ref.INT4, 64, counts, M, cols, rows)
+
+
 def test_matvec_rows_do_not_depend_on_their_neighbours_or_place():
     import torch
     import paper_2605_05888_amd as hub
