@@ -291,8 +291,8 @@ struct GateUp {
         const uint32_t x_row = (uint32_t)g.x_cols * Form::kElt;
         c.set_acts({static_cast<const unsigned char *>(g.x), (uint32_t)l.N * x_row, 0, 0, rows},
                    [&](int r) { return lists.token[base + r] * x_row; });
-        c.line = g.h_lines * open_unit.part / parts;
-        c.end = g.h_lines * (open_unit.part + 1) / parts;
+        c.line = few_part_line<kForm>(g.h_lines, open_unit.part, parts);
+        c.end = few_part_line<kForm>(g.h_lines, open_unit.part + 1, parts);
         c.groups = c.end > c.line ? (c.end - c.line + kDepth - 1) / kDepth : 1;
         return true;
     }
@@ -373,8 +373,8 @@ struct Down {
         for (int p = 0; p < kCT; ++p)
             c.panel[p] = panel_of<kForm>(l.down, row + 16 * p, end, l.F, l.scale_cols_f);
         c.set_acts(few_activation<kForm>(g, lists, at, rows), [](int r) { return r * (8u * Form::kElt); });
-        c.line = g.f_lines * open_unit.part / g.down_parts;
-        c.end = g.f_lines * (open_unit.part + 1) / g.down_parts;
+        c.line = few_part_line<kForm>(g.f_lines, open_unit.part, g.down_parts);
+        c.end = few_part_line<kForm>(g.f_lines, open_unit.part + 1, g.down_parts);
         c.groups = c.end > c.line ? (c.end - c.line + kDepth - 1) / kDepth : 1;
         return true;
     }

@@ -251,6 +251,20 @@ struct FewScales {
     }
 };
 
+// Two lines of a panel that were fetched as its upper and its lower eight rows, each 128 bytes (32 lanes the first 64 of all,
+// 32 the others): as lines.
+template <int kForm, int kTT, int kCT>
+__device__ __forceinline__ void few_to_lines(FewOperands<kForm, kTT, kCT> &first, FewOperands<kForm, kTT, kCT> &second)
+{
+#pragma unroll
+    for (int c = 0; c < kCT; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const auto v = __builtin_amdgcn_permlane32_swap(first.w[c][0][j], second.w[c][0][j], false, false);
+            first.w[c][0][j] = v[0], second.w[c][0][j] = v[1];
+        }
+}
+
 // What a lane has fetched, to the lane whose operand it is.
 __device__ __forceinline__ void from_lane(u32x4 &v, int from)
 {
@@ -445,6 +459,34 @@ struct FewCursor {
     }
 };
 
+// Lines in flight per wavefront: what 256 registers hold beside a line's products (registers of a line in the comment).
+template <int kForm, int kTT, int kCT>
+constexpr int few_depth()
+{
+    if (FewForm<kForm>::kQ4) // 4 kCT + 4, 16, 32
+        return kTT == 0 ? (FewForm<kForm>::kInt4 && kCT == 2 ? 4 : 8) : kTT == 1 ? 4 : 2;
+    return kTT <= 1 ? (kCT == 1 ? 8 : 4) : kCT == 1 ? 4 : 3; // 8 kCT + 4, 8, 16
+}
+
+// 4-bit lines are half a cache line.  Where there is depth for it they are fetched in pairs, eight rows of 128 bytes a load: a
+// cache line that is asked for by two loads, the second before it has arrived, holds both up (8 tokens of 256 experts int4
+// 289 us, in pairs 261).
+template <int kForm>
+constexpr bool few_pairs(int depth)
+{
+    return FewForm<kForm>::kQ4 && depth >= 4;
+}
+
+// First line of part `part` of `parts` of a reduction (of part `parts`: its end).  Pairs are in one part.
+template <int kForm>
+__device__ __forceinline__ int few_part_line(int lines, int part, int parts)
+{
+    if constexpr (!FewForm<kForm>::kQ4)
+        return lines * part / parts;
+    const int line = (lines + 1) / 2 * part / parts * 2;
+    return line < lines ? line : lines;
+}
+
 // A wavefront's stream: segment after segment (a panel of weight rows with the activation rows that meet it, some lines of
 // both), without a gap in the loads between them.  The source says what they are:
 //   open(cursor)    sets the cursor to the next segment, with at least one group of kDepth lines (lines past its end read as
@@ -462,17 +504,20 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
     if (!source.open(c))
         return;
     const int i = threadIdx.x % kWave / 4, q = threadIdx.x % 4; // whose operand this lane fetches
-    const uint32_t w_off = (uint32_t)i * (uint32_t)Form::row_bytes(g.cols) + (uint32_t)q * 16u;
+    constexpr bool kPairs = few_pairs<kForm>(kDepth);
+    const uint32_t row_bytes = (uint32_t)Form::row_bytes(g.cols);
+    const uint32_t w_off = kPairs ? (uint32_t)(i % 8) * row_bytes + (uint32_t)(i / 8 * 64 + q * 16) : (uint32_t)i * row_bytes + (uint32_t)q * 16u;
     constexpr int kFours = Form::kQ4 ? (kDepth + 3) / 4 : 1; // scale loads per group of lines
     FewScales<kForm, kCT> scales[kFours];
-    auto fetch = [&](Ops &o) {
-        const bool there = c.line < c.end; // (else no bytes: zeros, and the number of loads in flight stays)
+    auto fetch = [&](Ops &o, int d) {
+        const int odd = kPairs ? d % 2 : 0;
+        const bool there = c.line < c.end, w_there = c.line - odd < c.end; // (else no bytes: zeros, and the number of loads in flight stays)
 #pragma unroll
         for (int p = 0; p < kCT; ++p) {
-            const auto rw = few_buffer(c.panel[p].data, there ? c.panel[p].bytes : 0u);
+            const auto rw = few_buffer(c.panel[p].data, w_there ? c.panel[p].bytes : 0u);
 #pragma unroll
             for (int s = 0; s < Form::kLoads; ++s) {
-                uint32_t at = w_off + (uint32_t)(c.line * Form::kLineBytes + 64 * s);
+                uint32_t at = w_off + (uint32_t)((c.line - odd) * Form::kLineBytes + 64 * s) + (odd ? 8 * row_bytes : 0u);
                 if constexpr (kForm == kFewF32) // (past the row's end: the next row's, whose infinities and NaN stay its own)
                     at |= c.line * Form::kLineCols + 16 * s + 4 * q < g.cols ? 0u : kNowhere;
                 o.w[p][s] = __builtin_amdgcn_raw_buffer_load_b128(rw, (int)at, 0, 0);
@@ -529,9 +574,11 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
     fetch_scales();
 #pragma unroll
     for (int d = 0; d < kDepth; ++d)
-        fetch(o[d]);
+        fetch(o[d], d);
     FewSums<kForm, kTT, kCT> sums;
     sums.clear();
+    if constexpr (kPairs)
+        few_to_lines(o[0], o[1]);
     to_operand_lanes<kForm, kTT, kCT, kActs>(o[0]);
     for (;;) {
         if (--c.groups == 0) { // the next group is another segment's
@@ -551,16 +598,16 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
         fetch_scales();
 #pragma unroll
         for (int d = 0; d < kDepth; ++d) {
-            // (a line changes lanes under the products of the one before; a single line's ring has no such line)
-            if constexpr (kDepth > 1) {
-                to_operand_lanes<kForm, kTT, kCT, kActs>(o[(d + 1) % kDepth]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            // (a line changes lanes under the products of the one before)
+            const int next = (d + 1) % kDepth;
+            if constexpr (kPairs)
+                if (next % 2 == 0)
+                    few_to_lines(o[next], o[next + 1]);
+            to_operand_lanes<kForm, kTT, kCT, kActs>(o[next]);
+            __builtin_amdgcn_sched_barrier(0);
             few_multiply<kForm, kTT, kCT, kActs>(sums, o[d], scales[Form::kQ4 ? d / 4 : 0], d % 4);
             __builtin_amdgcn_sched_barrier(0);
-            fetch(o[d]);
-            if constexpr (kDepth == 1)
-                to_operand_lanes<kForm, kTT, kCT, kActs>(o[0]);
+            fetch(o[d], d);
         }
         if (--left == 0) {
             source.close(sums);
@@ -570,15 +617,6 @@ __device__ __forceinline__ void few_stream(Source &source, const FewCols &g)
             left = next;
         }
     }
-}
-
-// Lines in flight per wavefront: what 256 registers hold beside a line's products (registers of a line in the comment).
-template <int kForm, int kTT, int kCT>
-constexpr int few_depth()
-{
-    if (FewForm<kForm>::kQ4) // 4 kCT + 4, 16, 32
-        return kTT == 0 ? (FewForm<kForm>::kInt4 && kCT == 2 ? 4 : 8) : kTT == 1 ? 4 : 2;
-    return kTT <= 1 ? (kCT == 1 ? 8 : 4) : kCT == 1 ? 4 : 3; // 8 kCT + 4, 8, 16
 }
 
 // LDS and register barrier without the memory fence of __syncthreads, which would wait for the loads in flight.

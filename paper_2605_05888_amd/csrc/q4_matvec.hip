@@ -158,8 +158,8 @@ struct MatvecItems {
         const uint32_t x_row = (uint32_t)g.cols * Form::kElt;
         c.set_acts({static_cast<const unsigned char *>(g.x) + (int64_t)m0 * x_row, (uint32_t)rows * x_row, 0, 0, rows},
                    [&](int r) { return r * x_row; });
-        c.line = lines * open_unit.part / parts;
-        c.end = lines * (open_unit.part + 1) / parts;
+        c.line = few_part_line<kForm>(lines, open_unit.part, parts);
+        c.end = few_part_line<kForm>(lines, open_unit.part + 1, parts);
         c.groups = c.end > c.line ? (c.end - c.line + kDepth - 1) / kDepth : 1;
         return true;
     }
