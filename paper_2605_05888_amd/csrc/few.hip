@@ -171,9 +171,9 @@ int launch_layer_few(const FewArgs &args, int dtype, int format, hipStream_t st)
     // not fit in LDS
     const int64_t widest = rows * 32 <= kPoolFloats ? 32 : 16, rounds = ceil_div(args.H, widest * g.shares);
     g.down_cols = (int)(ceil_div(ceil_div(args.H, rounds * g.shares), 4) * 4);
-    // parts of an expert there: some eight units for each wavefront, none shorter than four lines
+    // parts of an expert there: some eight units for each wavefront, none shorter than eight lines (a ring of the fewest rows)
     const int row_floats = g.down_cols <= 16 ? 16 : 32;
-    for (g.down_parts = 1; g.down_parts < 16 && experts * g.down_parts < 8 * kFewWaves && g.f_lines >= 8 * g.down_parts &&
+    for (g.down_parts = 1; g.down_parts < 16 && experts * g.down_parts < 8 * kFewWaves && g.f_lines >= 16 * g.down_parts &&
                            2 * g.down_parts * rows * row_floats <= kPoolFloats;)
         g.down_parts *= 2;
     const char *const patience = getenv("MOE_FEW_PATIENCE"); // (tests: 0 makes every workgroup take over what is missing)
