@@ -132,21 +132,24 @@ size_t few_workspace_bytes(int64_t N, int64_t H, int E, int K, int64_t F, int dt
     return few_carve(nullptr, N, H, E, K, F, dtype).bytes;
 }
 
-// Width of the gate/up items and parts of their reduction: the least time of the longest share, in units of a line of one
-// column per wavefront.  Narrow items make even shares of little work (one token, 4 experts of 1408 columns: 22 columns per
-// workgroup, three items of 8 or two of 16), wide ones use their loads and registers better; parts do the same for the
-// wavefronts of a workgroup, at the price of an exchange and of groups that are not full.
-static void choose_items(FewKernelArgs &g, double experts)
+// Width of the gate/up items: the least time of the longest share, in units of a line of one column per wavefront, with the
+// parts that few_parts will choose about like here.  Narrow items make even shares of little work (one token, 4 experts of
+// 1408 columns: 22 columns per workgroup, three items of 8 or two of 16: 26.3 and 27.0 us for the second launch), wide ones use
+// their loads better (37 tokens of 32 experts fp4: 194 and 169 us), and in single precision the matrix instructions, half of
+// which 8 columns leave empty (5 tokens of 12 experts: 49 and 47 us), are the bound.
+static int choose_width(const FewKernelArgs &g, double experts, int narrowest)
 {
     int64_t least = INT64_MAX;
-    for (int width = 16; width >= 8; width -= 8)
+    int best = 16;
+    for (int width = 16; width >= narrowest; width /= 2)
         for (int parts = 1; parts <= kFewWaves && (parts == 1 || parts <= g.h_lines); parts *= 2) {
             const int64_t items = ceil_div((int64_t)(experts * (double)ceil_div(g.l.F, width) + 0.5), g.shares);
             const int64_t turns = ceil_div(items * parts, kFewWaves);
-            const int64_t time = turns * (ceil_div(ceil_div(g.h_lines, parts), 4) * 4 * (width + 4) + (parts > 1 ? 40 : 20));
+            const int64_t time = turns * (ceil_div(ceil_div(g.h_lines, parts), 4) * 4 * (width + 4) + (parts > 1 ? 12 : 8));
             if (time < least)
-                least = time, g.width = width;
+                least = time, best = width;
         }
+    return best;
 }
 
 int launch_layer_few(const FewArgs &args, int dtype, int format, hipStream_t st)
@@ -165,7 +168,7 @@ int launch_layer_few(const FewArgs &args, int dtype, int format, hipStream_t st)
     const int rows = args.N * args.K;
     const double touched = args.E * (1.0 - pow(1.0 - (double)args.K / args.E, args.N)); // experts, if all are equally popular
     const double experts = touched < 1.0 ? 1.0 : touched;
-    choose_items(g, experts);
+    g.width = choose_width(g, experts, dtype == MOE_BF16 ? 8 : 16);
     g.f_tiles = (int)ceil_div(args.F, g.width);
     // columns of a down tile: as many tiles as workgroups (or a multiple), none wider than 32, or 16 where the rows' sums would
     // not fit in LDS

@@ -362,7 +362,6 @@ __device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, con
                         all += v[t + u];
                     sums.one[c] = fmaf(scales.int4(c, d, t / kSame), all, sums.one[c]);
                 }
-                __builtin_amdgcn_sched_barrier(0); // (else the products of all tiles are alive at once)
             }
         } else {
             u32x4 codes[kCT];

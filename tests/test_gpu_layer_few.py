@@ -181,6 +181,25 @@ def test_equal_calls_give_equal_bits_whatever_the_workspace_held(form):
         assert torch.equal(t.call(), first), fill
 
 
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("N", [3, 21, 64])
+def test_shares_that_others_take_over_give_the_same_bits(form, N, monkeypatch):
+    """Without patience every workgroup does itself what it finds missing, beside the owner: the same values, twice."""
+    import torch
+    t = Layer(form, N, 192, 12, 3, 256, SOFT)
+    first = t.call().clone()
+    routed = t.idx.clone(), t.wt.clone()
+    monkeypatch.setenv("MOE_FEW_PATIENCE", "0")
+    for _ in range(3):
+        t.ws.fill_(0xFF)
+        t.out.fill_(0)
+        t.idx[:N] = -1
+        again = t.call()
+        torch.cuda.synchronize()
+        assert torch.equal(first.view(torch.uint8), again.view(torch.uint8))
+        assert torch.equal(routed[0], t.idx) and torch.equal(routed[1], t.wt)
+
+
 @pytest.mark.parametrize("form", ["bf16", (ref.FP4, 32)])
 def test_two_graphs_that_share_a_workspace(form):
     """Captured, replayed several times with eager work between; each replay takes what x holds then."""
