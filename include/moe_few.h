@@ -13,7 +13,8 @@
  *                their negatives; scale: one byte s that stands for 2^(s-127); group is 32
  *                (the OCP Microscaling format MXFP4).  Scale bytes 2 .. 252 are exact; below, small
  *                values may be flushed to zero, above, large ones overflow; 255 is not allowed.
- *   MOE_Q4_INT4  value = (code - 8) * scale; scale: bf16; group is 32, 64 or 128.
+ *   MOE_Q4_INT4  value = (code - 8) * scale; scale: bf16; group is 32, 64 or 128.  An infinity among the
+ *                activations may give NaN in its row where an infinity was due.
  * cols is a multiple of 64.  Codes and scales of several experts are stacked: [E, rows, cols/2].
  */
 #ifndef MOE_FEW_H
@@ -37,7 +38,8 @@ enum { MOE_FEW_TOKENS = 64 };
  *   out[n,:] = sum_k topk_w[n,k] * ( (silu(W_gate[e] x[n]) * (W_up[e] x[n])) W_down[e]^T ),  e = topk_idx[n,k]
  * Sums are fp32; the activation between the two products is rounded to dtype, and out once;
  * a row's contributions are not rounded before they are summed (moe_combine takes them in
- * dtype), so the result is the closer one.  Equal calls give equal bits.
+ * dtype), so the result is the closer one.  Equal calls give equal bits; a token's bits may
+ * depend on the tokens beside it (which decide how its sums are split).
  *   x [N,H] dtype    W_r [H,E] fp32    bias [E] fp32 or NULL
  *   W_gate, W_up [E,F,H], W_down [E,H,F] dtype
  *   topk_idx [N,K] int32 (out)    topk_w [N,K] fp32 (out)    out [N,H] dtype (out)
@@ -65,7 +67,7 @@ int moe_layer_few_q4(const void *x, int dtype, int64_t N, int64_t H, const float
  * Products of rows with 4-bit matrices: y[m,:] = x[m,:] W[e]^T for the rows m of
  * [seg_offsets[e], seg_offsets[e+1]), e < E_local, in fp32, rounded once.  With E_local == 1,
  * seg_offsets may be NULL: all M rows.  One launch, no workspace; made for a few rows per matrix
- * (the weights are read once per 64 rows of a segment).  Rows outside every segment are not written.
+ * (the weights are read once per 32 rows of a segment).  Rows outside every segment are not written.
  *   x [M,cols] dtype   codes [E_local,rows,cols/2]   scales [E_local,rows,ceil(cols/group)]   y [M,rows] dtype (out)
  *   seg_offsets [E_local+1] int32 ON THE DEVICE, non-decreasing, within [0,M]
  * MOE_BF16 only; rows a multiple of 8; cols below 2^21, rows below 2^27; E_local <= 65535.

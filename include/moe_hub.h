@@ -72,7 +72,7 @@ const char *moe_last_error(void);
  * use are ignored).  ROUTE: N*E fp32 logits (only when logits_opt is NULL).
  * DISPATCH_LAYOUT: per-chunk expert histograms.  GROUPED_FFN: the activation
  * a[M,F] between the two GEMMs plus the tile schedule.  LAYER_FEW (moe_few.h): parts of
- * the logits, the activation and the dependency counters.  Returns 0 on bad sizes. */
+ * the logits, a copy of x, the activation and the dependency counters.  Returns 0 on bad sizes. */
 size_t moe_workspace_bytes(int op, int64_t N, int64_t H, int E, int K, int G, int64_t F, int dtype);
 
 /*

@@ -1,9 +1,12 @@
 // The whole layer for a few tokens, in two launches.
 //
-//   few_logits   router logits, each as eight partial sums; clears the flags of the second launch
+//   few_logits   router logits, each as eight partial sums; clears the flags of the second launch; for 4-bit weights, x in the
+//                operands' order
 //   few_ffn      top-K, expert lists, both products of the experts that got a row, the weighted sum
 //
-// The layer is bound by reading the touched experts' weights once; everything else is latency.  few_ffn has one workgroup
+// The layer is bound by reading the touched experts' weights once (16 tokens of 256 experts of 7168 x 2048, bf16: 6.0 TB/s), with
+// 4 bits also by what few_stream.h says; everything else is latency (one token of 4 experts, 35 us in all: logits 5, top-K and
+// lists 3, gate/up 8 - 12, the flags 2, down 6, sums 3).  few_ffn has one workgroup
 // per compute unit, with a fixed share of each step:
 //   tokens   (more than kRouteAll) top-K of eight tokens, one per wavefront; up to kRouteAll tokens every workgroup selects
 //            for itself, which is quicker than waiting for another's answer

@@ -1,21 +1,23 @@
 // Products of a few rows with a panel of weight rows, as a stream of weights: what the decoding operators are made of.
 //
 // With a handful of rows a product is bound by reading the weights.  A wavefront reads lines of 64 (4 bits) or 128 bytes of
-// sixteen weight rows at a time, straight into registers in the operand layout of the matrix instructions, with kDepth
-// lines in flight; the activations of the same columns come beside them, from L2.  The matrix instructions are the cheap
-// part (an eighth of the time a line takes to arrive), also where most of their rows are empty.
+// sixteen weight rows at a time, straight into registers, with kDepth lines in flight; the activations of the same columns come
+// beside them, from L2.  In bf16 that runs at what panels of sixteen rows can be read with (5.4 - 6.2 TB/s, a large copy 6.7).
+// With 4 bits there are four times as many products, conversions and activations per byte, and they take about as long as the
+// reading: 37 tokens of 32 experts fp4 take 165 us, 135 without the activations and scales, 106 without the weights.
 //
-// The weights are the instruction's second operand, the activations the first: lane (q, i) = (lane / 16, lane % 16) holds
+// The weights are the matrix instruction's second operand, the activations the first: lane (q, i) = (lane / 16, lane % 16) holds
 // eight (fp32: four) columns of weight row i, and register r of a result belongs to activation row 4 q + r and weight row i.
 // Which columns of a line a lane holds is free as long as both operands agree.  A line has kChunks chunks, one operand
 // each; chunk t of lane q are the columns
-//   bf16   32 t +  8 q ..   two 16-byte loads per line, four lanes side by side read 64 bytes
+//   bf16   32 t +  8 q ..   two 16-byte loads per line
 //   fp32   16 t +  4 q ..   (four instructions of four columns each per chunk)
-//   4 bits 32 t +  8 q ..   one 16-byte load of columns 32 q .., then a transposition between the four lanes: an instruction
-//                           then covers one group of 32 columns, and four lanes side by side read 64 bytes of activations
+//   4 bits one 16-byte load holds columns 32 q ..; with activations in the same order (kOwn: 32 q + 8 t ..) that is it.  A group
+//          of 32 or 64 columns under one INT4 scale has to be in one instruction (32 t + 8 q ..), and so have activations in
+//          the caller's order: then four lanes transpose what they have.
 // FP4 codes become bf16 numbers times their scale on the way (a power of two: exact).  INT4: the scale is applied to an
 // instruction's sum in fp32 (a weight times its scale would have to be rounded).  A code c is the bf16 number 128 + c (a byte
-// beside 0x43); 136 times the sum of the activations, which an instruction with ones gives, is subtracted.
+// beside 0x43), so an instruction starts from -136 times the sum of the activations, which another one gives.
 // Scales are loaded for four lines at once, lane q those of line q: a load costs the address unit the same sixteen rows
 // whether it fetches a byte a row or sixteen (a byte per lane and line: the unit was busy 0.73 of the time).
 //
@@ -29,6 +31,8 @@
 // neighbouring lanes at a time: 64 bytes of one line in a cycle, or four lines in four (fetched like that, the unit was busy
 // 0.6 - 0.8 of the time).  So lane l fetches what lane (l % 4, l / 4) of the layout needs, four neighbours 64 bytes of a row,
 // and the registers change lanes on arrival (ds_bpermute).
+//
+// No register may be spilled: the compiler loses lanes of one that is (build.py refuses it), which sets the depths.
 #pragma once
 
 #include "common.h"
