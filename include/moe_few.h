@@ -43,6 +43,7 @@ enum { MOE_FEW_TOKENS = 64 };
  *   x [N,H] dtype    W_r [H,E] fp32    bias [E] fp32 or NULL
  *   W_gate, W_up [E,F,H], W_down [E,H,F] dtype
  *   topk_idx [N,K] int32 (out)    topk_w [N,K] fp32 (out)    out [N,H] dtype (out)
+ *   No output overlaps an input or another output.
  *   ws: moe_workspace_bytes(MOE_OP_LAYER_FEW, N, H, E, K, 0, F, dtype), 128-byte aligned; it needs no
  *   initialisation and may be used for anything else between calls.  Two calls that may overlap
  *   need a workspace each.

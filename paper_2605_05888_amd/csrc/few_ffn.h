@@ -336,6 +336,31 @@ struct GateUp {
     }
 };
 
+// All threads: the first weights of a down tile, columns [h0, h0 + cols) of the experts in their order, are asked for: kAhead cache
+// lines per thread, to be in L2 when the activation is complete (one token 35.6 -> 34.8 us, fp4 36.9 -> 36.0).  What is read is
+// nobody's result.
+constexpr int kAhead = 2;
+template <int kForm>
+__device__ __forceinline__ void few_ask_ahead(const FewKernelArgs &g, const FewLists &lists, int h0, int cols, uint32_t got[kAhead])
+{
+    constexpr int kScaleBytes = kForm == kFewFp4 ? 1 : 2;
+    const FewArgs &l = g.l;
+    const uint32_t bytes = (uint32_t)(cols * FewForm<kForm>::row_bytes(l.F)), scale_bytes = FewForm<kForm>::kQ4 ? cols * l.scale_cols_f * kScaleBytes : 0;
+    const uint32_t lines = (bytes + 127) / 128, each = lines + (scale_bytes + 127) / 128;
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+        const uint32_t u = a * kFewThreads + threadIdx.x, at = u / each, line = u % each;
+        got[a] = 0;
+        if (at < (uint32_t)lists.begin[3]) {
+            const int64_t row = (int64_t)lists.expert[at] * l.H + h0;
+            if (line < lines)
+                got[a] = (static_cast<const unsigned char *>(l.down.data) + row * FewForm<kForm>::row_bytes(l.F))[line * 128];
+            else
+                got[a] = (static_cast<const unsigned char *>(l.down.scales) + row * l.scale_cols_f * kScaleBytes)[(line - lines) * 128];
+        }
+    }
+}
+
 // A class's part of a down tile, columns [h0, h0 + cols).  A unit is one of `down_parts` parts of an expert's reduction; its
 // rows go to LDS by part and slot.
 template <int kForm, int kTT, int kCT>
@@ -485,9 +510,15 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
         if constexpr (kMaxTT > 1)
             gate_up(std::integral_constant<int, 2>{}, 2);
         few_signal(share_flags + who);
-        if ((int)blockIdx.x * g.down_cols >= l.H)
+        const int h0 = (int)blockIdx.x * g.down_cols;
+        if (h0 >= l.H)
             return;
+        uint32_t got[kAhead];
+        few_ask_ahead<kForm>(g, lists, h0, l.H - h0 < g.down_cols ? l.H - h0 : g.down_cols, got);
         who = few_missing(share_flags, g.shares, g.patience, box);
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a)
+            asm volatile("" ::"v"(got[a])); // (the loads are wanted)
         if (who < 0)
             break;
     }
