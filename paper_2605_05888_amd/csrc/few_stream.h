@@ -707,6 +707,7 @@ struct FewJoin {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (lane == 0) {
             room.parts_done[place] = 0;
+            asm volatile("" ::: "memory"); // (before the place is given away)
             __hip_atomic_store(&room.item[place], n + places, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
         }
     }
