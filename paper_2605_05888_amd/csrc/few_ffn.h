@@ -8,8 +8,8 @@
 // 4 bits also by what few_stream.h says; everything else is latency (one token of 4 experts, 35 us in all: logits 5, top-K and
 // lists 3, gate/up 8 - 12, the flags 2, down 6, sums 3).  few_ffn has one workgroup
 // per compute unit, with a fixed share of each step:
-//   tokens   (more than kRouteAll) top-K of eight tokens, one per wavefront; up to kRouteAll tokens every workgroup selects
-//            for itself, which is quicker than waiting for another's answer
+//   tokens   (more than few_route_all says) top-K of eight tokens, one per wavefront; of fewer every workgroup selects for
+//            itself, which is quicker than waiting for another's answer
 //   gate/up  items (expert, a few columns of F): both products of the expert's rows and the activation, into the workspace
 //   down     a few columns of H over ALL touched experts (as many as make a share for every workgroup): a token's sum over
 //            its K experts is made in one workgroup, in ascending k, so there is no third exchange
@@ -40,7 +40,6 @@
 namespace moe {
 
 constexpr int kParts = 8; // partial sums of a logit between the launches
-constexpr int kRouteAll = 8;
 constexpr int kMaxTokens = MOE_FEW_TOKENS, kMaxRows = kMaxTokens * (int)MOE_MAX_TOPK;
 constexpr int kMaxShares = 1024, kFlags = 32 + kMaxShares; // tokens', then shares'
 constexpr int kDefaultPatience = 1 << 15; // polls (about a microsecond each): longer than a share takes
@@ -86,6 +85,10 @@ __device__ __forceinline__ Pick few_select(const FewKernelArgs &g, int n)
            : l.E <= 4 * kWave ? select_top<4>(logit_of, l.E, l.K, l.score_mode)
                               : select_top<MOE_MAX_EXPERTS / kWave>(logit_of, l.E, l.K, l.score_mode);
 }
+
+// One token per wavefront, or two where a lane has one logit (9 tokens of 16 experts 28.6 -> 27.5 us, 16 of 64 48.1 -> 47.4; but
+// 16 of 256 51.7 -> 53.1, three per wavefront 24 of 32 38.7 -> 38.8).
+__device__ __forceinline__ bool few_route_all(const FewArgs &l) { return l.N <= (l.E <= kWave ? 2 : 1) * kFewWaves; }
 
 // The experts that got a row, by class and in ascending order within it, and their rows: slots from base on.  An expert with
 // more than a stream's rows (N K / 33 experts at most) is there twice: with that many, and with the rest.
@@ -440,7 +443,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     for (int e = threadIdx.x; e < l.E; e += kFewThreads)
         sh.routing.mask[e] = 0;
-    if (l.N <= kRouteAll) {
+    if (few_route_all(l)) {
         for (int n = wave; n < l.N; n += kFewWaves) {
             const Pick p = few_select(g, n);
             if (lane < l.K) {
