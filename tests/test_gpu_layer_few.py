@@ -200,6 +200,28 @@ def test_shares_that_others_take_over_give_the_same_bits(form, N, monkeypatch):
         assert torch.equal(routed[0], t.idx) and torch.equal(routed[1], t.wt)
 
 
+@pytest.mark.parametrize("form", ["bf16", "f32", (ref.FP4, 32), (ref.INT4, 64)])
+@pytest.mark.parametrize("N,E,K", [(1, 4, 2), (12, 8, 2), (64, 8, 2)])
+def test_calls_that_follow_each_other_on_one_workspace(form, N, E, K):
+    """Other tokens meet the same weights in the same workspace, without a wait between the calls: nothing of an earlier
+    call's activation, read by another part of the chip, is seen."""
+    import torch
+    t = Layer(form, N, 1024, E, K, 512)
+    xs = [t.d["x"]] + [torch.randn_like(t.d["x"]) for _ in range(2)]
+    want = []
+    for x in xs:
+        t.d["x"] = x
+        want.append(t.call(ws=torch.zeros_like(t.ws[:-64]), out=torch.empty_like(t.out[:N])))
+    torch.cuda.synchronize()
+    got = []
+    for turn in range(30):
+        t.d["x"] = xs[turn * turn % 3 if turn % 5 else 2]
+        got.append((turn * turn % 3 if turn % 5 else 2, t.call(out=torch.empty_like(t.out[:N]))))
+    torch.cuda.synchronize()
+    for which, out in got:
+        assert torch.equal(out.view(torch.uint8), want[which].view(torch.uint8))
+
+
 @pytest.mark.parametrize("form", ["bf16", (ref.FP4, 32)])
 def test_two_graphs_that_share_a_workspace(form):
     """Captured, replayed several times with eager work between; each replay takes what x holds then."""
