@@ -16,8 +16,10 @@
 //          of 32 or 64 columns under one INT4 scale has to be in one instruction (32 t + 8 q ..), and so have activations in
 //          the caller's order: then four lanes transpose what they have.
 // FP4 codes become bf16 numbers times their scale on the way (a power of two: exact).  INT4: the scale is applied to an
-// instruction's sum in fp32 (a weight times its scale would have to be rounded).  A code c is the bf16 number 128 + c (a byte
-// beside 0x43), so an instruction starts from -136 times the sum of the activations, which another one gives.
+// instruction's sum in fp32 (a weight times its scale would have to be rounded).  A code c becomes the bf16 number c 2^-12, so an
+// instruction starts from -8 2^-12 times the sum of the activations, which another one gives: sums hold up to 15 and 8 scales
+// of a weight that is at most 8.  (c - 8 itself takes seven instructions more for eight codes: 8 tokens of 256 experts 268 ->
+// 318 us.)  With the 2^-12, which the whole sum takes back at its end, 128 columns of the largest activations have finite sums.
 // Scales are loaded for four lines at once, lane q those of line q: a load costs the address unit the same sixteen rows
 // whether it fetches a byte a row or sixteen (a byte per lane and line: the unit was busy 0.73 of the time).
 //
@@ -135,6 +137,8 @@ struct FewOperands {
     u32x4 a[kRows][kActs];
 };
 
+constexpr float kInt4Unit = 0x1p-12f; // of INT4 operands
+
 template <int kForm, int kTT, int kCT>
 struct FewSums {
     static constexpr int kRows = kTT ? kTT : 1;
@@ -160,7 +164,9 @@ struct FewSums {
     __device__ __forceinline__ float value(int c, int v) const
     {
         if constexpr (kScalar)
-            return one[c];
+            return one[c] * (1.0f / kInt4Unit);
+        else if constexpr (FewForm<kForm>::kInt4)
+            return acc[v / 4][c][0][v % 4] * (1.0f / kInt4Unit);
         else if constexpr (kTT > 0)
             return acc[v / 4][c][0][v % 4];
         else if constexpr (kParts == 4)
@@ -181,14 +187,17 @@ __device__ __forceinline__ bf16x8 fp4_operand(uint32_t codes, float scale)
     return __builtin_bit_cast(bf16x8, r);
 }
 
-// Eight INT4 codes as bf16 numbers 128 + c, in the order of columns 0, 2, 4, 6, 1, 3, 5, 7 (int4_order gives the
-// activations the same).
+// Eight INT4 codes as bf16 numbers c kInt4Unit, in the order of columns 0, 2, 4, 6, 1, 3, 5, 7 (int4_order gives the
+// activations the same).  A byte from 0 to 15 is that many 2^-9 as an e4m3 number.
 __device__ __forceinline__ bf16x8 int4_operand(uint32_t codes)
 {
-    const uint32_t even = codes & 0x0F0F0F0Fu, odd = (codes >> 4) & 0x0F0F0F0Fu, high = 0x43434343u;
-    // byte selectors 0 - 3: of the second operand, 4 - 7: of the first
-    const u32x4 r = {__builtin_amdgcn_perm(high, even, 0x04010400u), __builtin_amdgcn_perm(high, even, 0x04030402u),
-                     __builtin_amdgcn_perm(high, odd, 0x04010400u), __builtin_amdgcn_perm(high, odd, 0x04030402u)};
+    const uint32_t even = codes & 0x0F0F0F0Fu, odd = codes >> 4 & 0x0F0F0F0Fu;
+    constexpr float scale = kInt4Unit * 0x1p9f;
+    u32x4 r;
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(even, scale, false));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(even, scale, true));
+    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(odd, scale, false));
+    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(odd, scale, true));
     return __builtin_bit_cast(bf16x8, r);
 }
 __device__ __forceinline__ bf16x8 int4_order(u32x4 a)
@@ -344,9 +353,10 @@ __device__ __forceinline__ void few_multiply(FewSums<kForm, kTT, kCT> &sums, con
                 }
             }
     } else {
-        // -136 times the activations' sum is where an instruction starts from
+        // -8 units times the activations' sum is where an instruction starts from
         constexpr int kSame = Form::kSame;
-        const bf16x8 minus = __builtin_bit_cast(bf16x8, u32x4{0xC308C308u, 0xC308C308u, 0xC308C308u, 0xC308C308u});
+        static_assert(kInt4Unit == 0x1p-12f);
+        const bf16x8 minus = __builtin_bit_cast(bf16x8, u32x4{0xBB00BB00u, 0xBB00BB00u, 0xBB00BB00u, 0xBB00BB00u}); // -2^-9
         auto act = [&](const u32x4 &a) { return kPacked ? __builtin_bit_cast(bf16x8, a) : int4_order(a); };
         if constexpr (kTT == 0) {
             const bf16x8 a = act(o.a[0][0]);
