@@ -72,6 +72,7 @@ int moe_layer_few_q4(const void *x, int dtype, int64_t N, int64_t H, const float
  *   x [M,cols] dtype   codes [E_local,rows,cols/2]   scales [E_local,rows,ceil(cols/group)]   y [M,rows] dtype (out)
  *   seg_offsets [E_local+1] int32 ON THE DEVICE, non-decreasing, within [0,M]
  * MOE_BF16 only; rows a multiple of 8; cols below 2^21, rows below 2^27; E_local <= 65535.
+ * An offset outside [0,M] counts as the nearer end; where offsets decrease, some or all segments are not computed.
  */
 int moe_matvec_q4(const void *x, int dtype, int64_t M, int64_t cols, int64_t rows, int E_local, const int32_t *seg_offsets,
                   int format, int group, const void *codes, const void *scales, void *y, void *stream);

@@ -24,20 +24,27 @@ struct MatvecLists {
     int wave_full[kFewWaves], wave_part[kFewWaves];
 };
 
-// All threads: of segments [e0, e0 + E).
+// All threads: of segments [e0, e0 + E).  Offsets are taken into [0, M]; where they decrease there are no entries, so that no
+// more rows are listed than there are.
 template <int kForm>
 __device__ __forceinline__ void matvec_lists(MatvecLists &lists, const MatvecArgs &g, int e0, int E)
 {
     constexpr int kPer = kMvSegments / kFewThreads;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     int full[kPer], fulls = 0, parts = 0; // parts: of class 1 above 16 bits of class 0
-    int part[kPer];
+    int part[kPer], falls = 0;
+    const int M = (int)g.M;
+    auto offset = [&](int e) {
+        const int m = g.seg_offsets ? g.seg_offsets[e] : e ? M : 0;
+        return m < 0 ? 0 : m < M ? m : M;
+    };
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int e = threadIdx.x * kPer + i;
         full[i] = part[i] = 0;
         if (e < E) {
-            const int m0 = g.seg_offsets ? g.seg_offsets[e0 + e] : 0, m1 = g.seg_offsets ? g.seg_offsets[e0 + e + 1] : (int)g.M;
+            const int m0 = offset(e0 + e), m1 = offset(e0 + e + 1);
+            falls |= m1 < m0;
             const int rows = m1 > m0 ? m1 - m0 : 0, left = rows % kFewMost;
             lists.begin[e] = m0;
             if (e == E - 1)
@@ -59,7 +66,7 @@ __device__ __forceinline__ void matvec_lists(MatvecLists &lists, const MatvecArg
         lists.wave_full[wave] = fulls;
         lists.wave_part[wave] = parts;
     }
-    __syncthreads();
+    falls = __syncthreads_or(falls);
     at += fulls;
     place += parts;
     int all = 0, all_parts = 0;
@@ -86,9 +93,9 @@ __device__ __forceinline__ void matvec_lists(MatvecLists &lists, const MatvecArg
     }
     if (threadIdx.x == 0) {
         lists.full[E] = all;
-        lists.entries[0] = all_parts & 0xFFFF;
-        lists.entries[1] = all_parts >> 16;
-        lists.entries[2] = all;
+        lists.entries[0] = falls ? 0 : all_parts & 0xFFFF;
+        lists.entries[1] = falls ? 0 : all_parts >> 16;
+        lists.entries[2] = falls ? 0 : all;
     }
     __syncthreads();
 }
