@@ -1,6 +1,7 @@
 // The whole layer for a few tokens: router logits and the launches (few_ffn.h has the rest of the layer).
 #include <math.h>
-#include <stdlib.h>
+
+#include <atomic>
 
 #include "common.h"
 #include "few.h"
@@ -152,6 +153,9 @@ static int choose_width(const FewKernelArgs &g, double experts, int narrowest)
     return best;
 }
 
+static std::atomic<int> test_polls{-1};
+extern "C" void moe_few_test_waits(int polls) { test_polls.store(polls, std::memory_order_relaxed); }
+
 int launch_layer_few(const FewArgs &args, int dtype, int format, hipStream_t st)
 {
     const FewWorkspace w = few_carve(args.ws, args.N, args.H, args.E, args.K, args.F, dtype);
@@ -179,8 +183,8 @@ int launch_layer_few(const FewArgs &args, int dtype, int format, hipStream_t st)
     for (g.down_parts = 1; g.down_parts < 16 && experts * g.down_parts < 8 * kFewWaves && g.f_lines >= 16 * g.down_parts &&
                            2 * g.down_parts * rows * row_floats <= kPoolFloats;)
         g.down_parts *= 2;
-    const char *const patience = getenv("MOE_FEW_PATIENCE"); // (tests: 0 makes every workgroup take over what is missing)
-    g.patience = patience ? atoi(patience) : kDefaultPatience;
+    const int polls = test_polls.load(std::memory_order_relaxed);
+    g.patience = polls < 0 ? kDefaultPatience : polls;
     const bool packed = format != kNoFormat;
     g.x = packed ? w.x : args.x;
     g.x_cols = packed ? g.h_lines * 128 : args.H;
