@@ -37,8 +37,9 @@ struct MatvecArgs {
 };
 
 // Not part of the interface: what tests make of a wait of moe_layer_few.  polls: how often it looks before it takes over what
-// is missing (0: at once; negative: as the library has it).
-extern "C" void moe_few_test_waits(int polls);
+// is missing (0: at once; negative: as the library has it).  workgroups: how many are launched; fewer than one per compute unit
+// (0: that) are what a call has while others hold the compute units.
+extern "C" void moe_few_test_waits(int polls, int workgroups);
 
 size_t few_workspace_bytes(int64_t N, int64_t H, int E, int K, int64_t F, int dtype);
 int launch_layer_few(const FewArgs &args, int dtype, int format, hipStream_t st);

@@ -153,8 +153,20 @@ static int choose_width(const FewKernelArgs &g, double experts, int narrowest)
     return best;
 }
 
-static std::atomic<int> test_polls{-1};
-extern "C" void moe_few_test_waits(int polls) { test_polls.store(polls, std::memory_order_relaxed); }
+// Polls (about a microsecond each) that a workgroup waits for others' shares: a quarter of a millisecond, and what the largest
+// share's weights take at 8 GB/s, a third of a compute unit's part of the memory's rate.
+static int choose_patience(const FewKernelArgs &g, double experts, int64_t row_bytes)
+{
+    const double items = ceil(experts * (double)g.f_tiles / g.shares);
+    return (int)fmin(250.0 + items * 2.0 * g.width * (double)row_bytes / 8e3, 1e6);
+}
+
+static std::atomic<int> test_polls{-1}, test_workgroups{0};
+extern "C" void moe_few_test_waits(int polls, int workgroups)
+{
+    test_polls.store(polls, std::memory_order_relaxed);
+    test_workgroups.store(workgroups, std::memory_order_relaxed);
+}
 
 int launch_layer_few(const FewArgs &args, int dtype, int format, hipStream_t st)
 {
@@ -184,7 +196,10 @@ int launch_layer_few(const FewArgs &args, int dtype, int format, hipStream_t st)
                            2 * g.down_parts * rows * row_floats <= kPoolFloats;)
         g.down_parts *= 2;
     const int polls = test_polls.load(std::memory_order_relaxed);
-    g.patience = polls < 0 ? kDefaultPatience : polls;
+    const int64_t row_bytes = format != kNoFormat ? args.H / 2 : (int64_t)args.H * (dtype == MOE_BF16 ? 2 : 4);
+    g.patience = polls < 0 ? choose_patience(g, rows < args.E ? rows : args.E, row_bytes) : polls;
+    const int workgroups = test_workgroups.load(std::memory_order_relaxed);
+    g.workgroups = workgroups > 0 && workgroups < g.shares ? workgroups : g.shares;
     const bool packed = format != kNoFormat;
     g.x = packed ? w.x : args.x;
     g.x_cols = packed ? g.h_lines * 128 : args.H;

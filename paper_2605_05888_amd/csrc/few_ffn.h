@@ -20,8 +20,10 @@
 // one in 12 ns (512 workgroups that drew from one counter and polled another: one token 64 us instead of 27).
 //
 // What a step needs from other workgroups is said by a flag per share.  A workgroup that has waited for longer than any share
-// takes does the missing share itself (a second time, with the same bits, if its owner is only late): every wait ends, however
-// few workgroups of the grid are resident, several calls on several streams included.
+// takes does a missing share itself (a second time, with the same bits, if its owner is only late), and another one as long as
+// one is missing, without a wait between them: every wait ends, however few workgroups of the grid are resident, several calls
+// on several streams included.  Workgroups that wait take different shares (the first missing one, the second, ..., by their own
+// number), so that together they need about missing / waiting turns (3 tokens, H = 192: 0.25 ms with 100 of 256 workgroups).
 // The activation goes from XCD to XCD.  It is written through and a share's flag is set once its stores are acknowledged.  It
 // is read by ordinary loads: a cache line belongs to one item, so no XCD can hold one that was read or written in part before
 // its item was complete.  (Telling the caches to drop what they hold takes 5 - 9 us.)
@@ -42,7 +44,6 @@ namespace moe {
 constexpr int kParts = 8; // partial sums of a logit between the launches
 constexpr int kMaxTokens = MOE_FEW_TOKENS, kMaxRows = kMaxTokens * (int)MOE_MAX_TOPK;
 constexpr int kMaxShares = 1024, kFlags = 32 + kMaxShares; // tokens', then shares'
-constexpr int kDefaultPatience = 1 << 15; // polls (about a microsecond each): longer than a share takes
 
 // ------------------------------------------------------------------------
 struct FewKernelArgs {
@@ -51,11 +52,12 @@ struct FewKernelArgs {
     const void *x; // as gate/up reads it: packed for 4-bit weights
     int x_cols;    // of a row of it
     uint32_t *flags;
+    int workgroups;
     int shares;    // of gate/up items
     int width;      // columns of F of an item: 8 or 16
     int down_cols;  // columns of H of a down tile, at most 16 kCT
     int down_parts; // of an expert's reduction there
-    int patience;
+    int patience; // polls of a wait
     int h_lines, f_lines, f_tiles; // lines of H and F; items of an expert
 };
 
@@ -201,30 +203,42 @@ __device__ __forceinline__ void few_make_lists(FewLists &lists, FewRouting &r, i
     __syncthreads();
 }
 
-// All threads: -1 once all flags are set, or one that still is not after `patience` polls.
-__device__ __forceinline__ int few_missing(const uint32_t *flags, int count, int patience, int *box)
+// All threads: -1 once all flags are set; if some still are not after `patience` polls, one of them: of m, the one that has
+// blockIdx.x % m before it.  After that `patience` is 0.  box: of at least count / 64 + 1.
+__device__ __forceinline__ int few_missing(const uint32_t *flags, int count, int &patience, uint64_t *box)
 {
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, words = (count + kWave - 1) / kWave;
     for (int poll = 0;; ++poll) {
-        int miss = 0x7FFFFFFF;
-        for (int i = threadIdx.x; i < count; i += kFewThreads)
-            if (__hip_atomic_load(flags + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 0)
-                miss = miss < i ? miss : i;
-        const uint64_t m = __ballot(miss != 0x7FFFFFFF);
-        const int mine = m ? __builtin_amdgcn_readlane(miss, __builtin_ctzll(m)) : 0x7FFFFFFF;
-        if (lane == 0)
-            box[wave] = mine;
+        for (int c = wave; c < words; c += kFewWaves) {
+            const int i = c * kWave + lane;
+            const uint64_t miss = __ballot(i < count && __hip_atomic_load(flags + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 0);
+            if (lane == 0)
+                box[c] = miss;
+        }
         few_barrier();
-        int first = 0x7FFFFFFF;
-#pragma unroll
-        for (int w = 0; w < kFewWaves; ++w)
-            first = first < box[w] ? first : box[w];
-        first = __builtin_amdgcn_readfirstlane(first);
+        const bool some = __ballot(lane < words && box[lane] != 0) != 0;
+        int found = -1;
+        if (some && poll >= patience) {
+            int m = 0;
+            for (int c = 0; c < words; ++c)
+                m += (int)__popcll(box[c]);
+            int before = (int)(blockIdx.x % (uint32_t)m);
+            for (int c = 0; c < words && found < 0; ++c) {
+                uint64_t left = box[c];
+                const int here = (int)__popcll(left);
+                if (before < here) {
+                    for (; before > 0; --before)
+                        left &= left - 1;
+                    found = c * kWave + (int)__builtin_ctzll(left);
+                }
+                before -= here;
+            }
+            patience = 0;
+        }
+        found = __builtin_amdgcn_readfirstlane(found);
         few_barrier();
-        if (first == 0x7FFFFFFF)
-            return -1;
-        if (poll >= patience)
-            return first;
+        if (!some || found >= 0)
+            return found;
         __builtin_amdgcn_s_sleep(4);
     }
 }
@@ -438,7 +452,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
     __shared__ FewLists lists;
     __shared__ FewRoom room;
     __shared__ int counters[3]; // units drawn, of each class
-    __shared__ int box[kFewWaves];
+    __shared__ uint64_t box[kMaxShares / kWave];
     const FewArgs &l = g.l;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     for (int e = threadIdx.x; e < l.E; e += kFewThreads)
@@ -457,6 +471,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
         }
     } else {
         const int groups = (l.N + kFewWaves - 1) / kFewWaves;
+        int patience = g.patience;
         for (int who = (int)blockIdx.x < groups ? (int)blockIdx.x : -1;;) {
             if (who >= 0) {
                 const int n = who * kFewWaves + wave;
@@ -469,7 +484,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
                 }
                 few_signal(g.flags + who);
             }
-            who = few_missing(g.flags, groups, g.patience, box);
+            who = few_missing(g.flags, groups, patience, box);
             if (who < 0)
                 break;
         }
@@ -493,6 +508,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
         few_barrier();
     };
     auto empty = [&](int cls) { return __builtin_amdgcn_readfirstlane(lists.begin[cls]) == __builtin_amdgcn_readfirstlane(lists.begin[cls + 1]); };
+    int patience = g.patience;
     for (int who = blockIdx.x;;) {
         int before = 0;
         restart();
@@ -518,7 +534,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
             return;
         uint32_t got[kAhead];
         few_ask_ahead<kForm>(g, lists, h0, l.H - h0 < g.down_cols ? l.H - h0 : g.down_cols, got);
-        who = few_missing(share_flags, g.shares, g.patience, box);
+        who = few_missing(share_flags, g.shares, patience, box);
 #pragma unroll
         for (int a = 0; a < kAhead; ++a)
             asm volatile("" ::"v"(got[a])); // (the loads are wanted)
@@ -572,7 +588,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void few_ffn(FewKernelArgs g)
 template <int kForm>
 void launch_few_ffn(const FewKernelArgs &g, hipStream_t st)
 {
-    const dim3 grid((unsigned)g.shares), block(kFewThreads);
+    const dim3 grid((unsigned)g.workgroups), block(kFewThreads);
     if (g.l.N <= 16) {
         if (g.down_cols <= 16)
             hipLaunchKernelGGL((few_ffn<kForm, 1, 1>), grid, block, 0, st, g);

@@ -9,14 +9,14 @@ pytestmark = pytest.mark.gpu
 
 
 @contextlib.contextmanager
-def waits(polls):
+def waits(polls, workgroups=0):
     import paper_2605_05888_amd as hub
     lib = hub.load_library()
-    lib.moe_few_test_waits(polls)
+    lib.moe_few_test_waits(polls, workgroups)
     try:
         yield
     finally:
-        lib.moe_few_test_waits(-1)
+        lib.moe_few_test_waits(-1, 0)
 
 
 @pytest.mark.parametrize("form", FORMS)
@@ -35,3 +35,30 @@ def test_shares_that_are_taken_over_at_once_give_the_same_bits(form, N):
             torch.cuda.synchronize()
             assert torch.equal(first.view(torch.uint8), again.view(torch.uint8))
             assert torch.equal(routed[0], t.idx) and torch.equal(routed[1], t.wt)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("N,H,F", [(3, 192, 1024), (40, 512, 640)])
+@pytest.mark.parametrize("workgroups", [1, 7, 100, 200])
+def test_a_call_with_few_workgroups_does_the_others_shares_in_parallel(form, N, H, F, workgroups):
+    """As where other work holds the compute units.  The waits of one share after the other, 33 ms each, took seconds; together
+    they take one wait, and a few turns."""
+    import torch
+    print("workgroups", form, N, H, F, workgroups, flush=True)
+    t = Layer(form, N, H, 12, 3, F, SOFT)
+    first = t.call().clone()
+    routed = t.idx.clone(), t.wt.clone()
+    start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    with waits(-1, workgroups):
+        for _ in range(2):
+            t.ws.fill_(0xFF)
+            t.out.fill_(0)
+            t.idx[:N] = -1
+            start.record()
+            again = t.call()
+            end.record()
+            torch.cuda.synchronize()
+            assert torch.equal(first.view(torch.uint8), again.view(torch.uint8))
+            assert torch.equal(routed[0], t.idx) and torch.equal(routed[1], t.wt)
+    print("ms", start.elapsed_time(end), flush=True)
+    assert start.elapsed_time(end) < 100.0
