@@ -650,7 +650,7 @@ static int check_q4_matrix(int dtype, int64_t rows, int64_t cols, int format, in
     MOE_TRY(check_dtype(dtype));
     MOE_TRY(check_q4(format, group));
     MOE_TRY(check_q4_cols(cols, (int64_t)1 << 22));
-    if (rows < 0 || rows > ((int64_t)1 << 36) / (cols + group))
+    if (rows < 0 || rows > (((int64_t)1 << 36) - 1) / cols)
         return fail(MOE_ERR_ARG, "rows must be >= 0 and rows * cols below 2^36 (got rows=%lld, cols=%lld)", (long long)rows,
                     (long long)cols);
     return MOE_OK;

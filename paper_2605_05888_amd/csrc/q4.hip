@@ -208,9 +208,9 @@ static Q4Args q4_args(int64_t rows, int64_t cols, int group)
     Q4Args g = {};
     g.rows = rows;
     g.cols = (int)cols;
-    g.group = group;
+    g.group = cols < group ? (int)cols : group; // (64 columns under a scale for 128: as many lanes as there are columns)
     g.scale_cols = (int)q4_scale_cols(cols, group);
-    g.units = g.scale_cols * (group / 8);
+    g.units = g.scale_cols * (g.group / 8); // (at most 4/3 of the columns: a grid for 2^36 has fewer than 2^32 threads)
     return g;
 }
 
