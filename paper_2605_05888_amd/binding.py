@@ -368,6 +368,13 @@ def _need_shape(t, dtype, shape, name):
         raise TypeError(f"{name} is on another device than the current one")
 
 
+def _few_ws_args(ws):
+    """A workspace that kernels of the current device can write; None is left for the library to refuse."""
+    if ws is not None:
+        _need_shape(ws, ws.dtype, tuple(ws.shape), "ws")
+    return _ws_args(ws)
+
+
 def _need_q4(codes, scales, rows_shape, cols, fmt, group, name):
     if fmt not in (Q4_FP4, Q4_INT4) or group not in (32, 64, 128):
         raise ValueError(f"format must be Q4_FP4 or Q4_INT4 and group 32, 64 or 128, got {fmt} and {group}")
@@ -397,7 +404,7 @@ def moe_layer_few(x, W_r, bias, K: int, score_mode: int, W_gate, W_up, W_down, t
     _need_shape(W_gate, x.dtype, (E, F, H), "W_gate")
     _need_shape(W_up, x.dtype, (E, F, H), "W_up")
     _need_shape(W_down, x.dtype, (E, H, F), "W_down")
-    wp, wb = _ws_args(ws)
+    wp, wb = _few_ws_args(ws)
     lib = _lib or load_library()
     _check(lib.moe_layer_few(x.data_ptr(), code, N, H, W_r.data_ptr(), _ptr(bias), E, K, score_mode, F, W_gate.data_ptr(),
                              W_up.data_ptr(), W_down.data_ptr(), topk_idx.data_ptr(), topk_w.data_ptr(), out.data_ptr(), wp, wb,
@@ -411,7 +418,7 @@ def moe_layer_few_q4(x, W_r, bias, K: int, score_mode: int, gate, up, down, fmt:
     _need_q4(*gate, (E, F), H, fmt, group, "gate")
     _need_q4(*up, (E, F), H, fmt, group, "up")
     _need_q4(*down, (E, H), F, fmt, group, "down")
-    wp, wb = _ws_args(ws)
+    wp, wb = _few_ws_args(ws)
     lib = _lib or load_library()
     _check(lib.moe_layer_few_q4(x.data_ptr(), code, N, H, W_r.data_ptr(), _ptr(bias), E, K, score_mode, F, fmt, group,
                                 gate[0].data_ptr(), gate[1].data_ptr(), up[0].data_ptr(), up[1].data_ptr(), down[0].data_ptr(),
