@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+import few_close
 import few_reference as ref
 import moe_inputs as mi
 from test_gpu_layer_few import FORMS, SOFT, Layer
@@ -10,14 +11,6 @@ from test_gpu_q4 import FORMATS, dev, host
 pytestmark = pytest.mark.gpu
 
 MOST = 0x7F7F  # the largest bf16 number
-
-
-def held(packed, scales, fmt, group):
-    """What an fp32 sum holds of a weight: its magnitude, or (INT4) its code and 8 apart, in scales."""
-    if fmt == ref.FP4:
-        return np.abs(ref.values(packed, scales, fmt, group))
-    s = np.repeat(np.abs(ref.f64(scales)), group, axis=-1)[..., :2 * packed.shape[-1]]
-    return (ref.codes_of(packed) + 8.0) * s
 
 
 def large(rng, shape):
@@ -47,7 +40,7 @@ def test_products_of_the_largest_activations(fmt, group, M, cols, rows):
     x[M // 2] = MOST  # its sums over a group are the largest there are
     y = torch.zeros((M, rows), dtype=torch.bfloat16, device="cuda:0")
     hub.moe_matvec_q4(dev(x), None, dev(codes), dev(scales), fmt, group, y)
-    want, err = ref.product(ref.f64(x), ref.values(codes[0], scales[0], fmt, group), held(codes[0], scales[0], fmt, group))
+    want, err = ref.product(ref.f64(x), ref.values(codes[0], scales[0], fmt, group), few_close.held(codes[0], scales[0], fmt, group))
     ref.check(host(y), want, err + ref.HALF["bf16"] * (np.abs(want) + err), "large")
 
 
@@ -66,14 +59,14 @@ def test_products_of_the_smallest_activations(fmt, group, M):
     x = (rng.integers(1 << 7, 7 << 7, (M, cols)) | rng.integers(0, 2, (M, cols)) << 15).astype(np.uint16)
     y = torch.zeros((M, rows), dtype=torch.bfloat16, device="cuda:0")
     hub.moe_matvec_q4(dev(x), None, dev(codes), dev(scales), fmt, group, y)
-    want, err = ref.product(ref.f64(x), ref.values(codes[0], scales[0], fmt, group), held(codes[0], scales[0], fmt, group))
+    want, err = ref.product(ref.f64(x), ref.values(codes[0], scales[0], fmt, group), few_close.held(codes[0], scales[0], fmt, group))
     ref.check(host(y), want, err + ref.HALF["bf16"] * (np.abs(want) + err), "small")
 
 
 class CloseLayer(Layer):
     def matrix(self, which):
         w = self.w[which]
-        return lambda e: (ref.values(w[0][e], w[1][e], *self.form), held(w[0][e], w[1][e], *self.form))
+        return lambda e: (ref.values(w[0][e], w[1][e], *self.form), few_close.held(w[0][e], w[1][e], *self.form))
 
 
 @pytest.mark.parametrize("form", FORMATS)
