@@ -13,8 +13,9 @@
  *                their negatives; scale: one byte s that stands for 2^(s-127); group is 32
  *                (the OCP Microscaling format MXFP4).  Scale bytes 2 .. 252 are exact; below, small
  *                values may be flushed to zero, above, large ones overflow; 255 is not allowed.
- *   MOE_Q4_INT4  value = (code - 8) * scale; scale: bf16; group is 32, 64 or 128.  An infinity among the
- *                activations may give NaN in its row where an infinity was due.
+ *   MOE_Q4_INT4  value = (code - 8) * scale; scale: bf16; group is 32, 64 or 128.  Products sum code * x and
+ *                take off 8 * x once per group, so that an fp32 sum holds up to 23 scales of a weight; finite activations of any size are
+ *                summed without overflow, an infinity among them may give NaN in its row where an infinity was due.
  * cols is a multiple of 64.  Codes and scales of several experts are stacked: [E, rows, cols/2].
  */
 #ifndef MOE_FEW_H
@@ -33,7 +34,9 @@ enum { MOE_FEW_TOKENS = 64 };
 
 /*
  * The whole layer of Section II-A for N <= MOE_FEW_TOKENS tokens on one device that holds
- * every expert: routing, expert computation, combine and scaling.
+ * every expert: routing, expert computation, combine and scaling.  What it saves over the calls of moe_hub.h is launches and
+ * exchanges: a seventh to a third of the time for one token, nothing from about 16 tokens of large bf16 layers on, where it can
+ * take 8 % longer, nor in small fp32 layers (5 tokens of 12 experts of 516 x 1028: 12 % longer).
  *   picks and weights of token n: as moe_route gives them, bit for bit (topk_idx, topk_w)
  *   out[n,:] = sum_k topk_w[n,k] * ( (silu(W_gate[e] x[n]) * (W_up[e] x[n])) W_down[e]^T ),  e = topk_idx[n,k]
  * Sums are fp32; the activation between the two products is rounded to dtype, and out once;

@@ -316,7 +316,9 @@ struct GateUp {
         c.groups = c.end > c.line ? (c.end - c.line + kDepth - 1) / kDepth : 1;
         return true;
     }
-    // Value v of the lanes.
+    // Value v of the lanes.  In bf16 the activation is rounded to bf16 here, as moe_grouped_ffn rounds it: it is the down product's
+    // operand (a second number for the rest would double its loads and products), and a prompt's tokens and the next ones go
+    // through the same roundings.
     __device__ __forceinline__ void store(int v, float gate, float up) const
     {
         const float a = silu_mul_f32(gate, up);

@@ -2,7 +2,7 @@
 //
 // With a handful of rows a product is bound by reading the weights.  A wavefront reads lines of 64 (4 bits) or 128 bytes of
 // sixteen weight rows at a time, straight into registers, with kDepth lines in flight; the activations of the same columns come
-// beside them, from L2.  In bf16 that runs at what panels of sixteen rows can be read with (5.4 - 6.2 TB/s, a large copy 6.7).
+// beside them, from L2.  In bf16 that runs at what panels of sixteen rows can be read with (5.4 - 6.2 TB/s, one large read 6.7).
 // With 4 bits there are four times as many products, conversions and activations per byte, and they take about as long as the
 // reading: 37 tokens of 32 experts fp4 take 165 us, 135 without the activations and scales, 106 without the weights.
 //
