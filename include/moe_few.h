@@ -50,8 +50,8 @@ enum { MOE_FEW_TOKENS = 64 };
  *   ws: moe_workspace_bytes(MOE_OP_LAYER_FEW, N, H, E, K, 0, F, dtype), 128-byte aligned; it needs no
  *   initialisation and may be used for anything else between calls.  Two calls that may overlap
  *   need a workspace each.
- *   Where other work holds compute units, calls on other streams included, the workgroups that are on the device wait about a
- *   quarter of a millisecond, and some times what the layer takes, and then do the others' shares: same bits, no wait without end.
+ *   Where other work holds compute units, calls on other streams included, the workgroups that are on the device wait 60
+ *   microseconds, and up to three times what the layer takes, and then do the others' shares: same bits, no wait without end.
  * MOE_BF16: H and F multiples of 64.  MOE_F32: multiples of 4.  H, F below 2^21.
  */
 int moe_layer_few(const void *x, int dtype, int64_t N, int64_t H, const float *W_r, const float *bias, int E, int K,

@@ -153,12 +153,14 @@ static int choose_width(const FewKernelArgs &g, double experts, int narrowest)
     return best;
 }
 
-// Polls (about a microsecond each) that a workgroup waits for others' shares: a quarter of a millisecond, and what the largest
-// share's weights take at 8 GB/s, a third of a compute unit's part of the memory's rate.
+// Polls (about a microsecond each) that a workgroup waits for others' shares: 60, and what the largest share's weights take at
+// 8 GB/s, a third of a compute unit's part of the memory's rate.  That is longer than any share takes with the card to itself (the
+// layers alone take the same time with 30 and with 250) and shorter than much more work would be: one token of 4 experts on four
+// streams at once, 282 us for the four with 250, 192 with 60, 177 with 30; one after the other 139.
 static int choose_patience(const FewKernelArgs &g, double experts, int64_t row_bytes)
 {
     const double items = ceil(experts * (double)g.f_tiles / g.shares);
-    return (int)fmin(250.0 + items * 2.0 * g.width * (double)row_bytes / 8e3, 1e6);
+    return (int)fmin(60.0 + items * 2.0 * g.width * (double)row_bytes / 8e3, 1e6);
 }
 
 static std::atomic<int> test_polls{-1}, test_workgroups{0};

@@ -23,7 +23,7 @@
 // takes does a missing share itself (a second time, with the same bits, if its owner is only late), and another one as long as
 // one is missing, without a wait between them: every wait ends, however few workgroups of the grid are resident, several calls
 // on several streams included.  Workgroups that wait take different shares (the first missing one, the second, ..., by their own
-// number), so that together they need about missing / waiting turns (3 tokens, H = 192: 0.25 ms with 100 of 256 workgroups).
+// number), so that together they need about missing / waiting turns (3 tokens, H = 192: 0.11 ms with 100 of 256 workgroups).
 // The activation goes from XCD to XCD.  It is written through and a share's flag is set once its stores are acknowledged.  It
 // is read by ordinary loads: a cache line belongs to one item, so no XCD can hold one that was read or written in part before
 // its item was complete.  (Telling the caches to drop what they hold takes 5 - 9 us.)

@@ -62,3 +62,27 @@ def test_a_call_with_few_workgroups_does_the_others_shares_in_parallel(form, N, 
             assert torch.equal(routed[0], t.idx) and torch.equal(routed[1], t.wt)
     print("ms", start.elapsed_time(end), flush=True)
     assert start.elapsed_time(end) < 100.0
+
+
+def test_calls_on_several_streams_do_not_wait_for_each_other_for_long():
+    """Four streams of calls whose workgroups are on the device in part: a call is some tens of microseconds, and waits of 33 ms
+    for a share made it as many milliseconds."""
+    import time
+    import torch
+    layers = [Layer("bf16", n, 1024, 32, 4, 512, SOFT, seed=n) for n in (1, 1, 2, 5)]
+    streams = [torch.cuda.Stream() for _ in layers]
+    want = [t.call().clone() for t in layers]
+    torch.cuda.synchronize()
+    calls = 40
+    for turn in range(2):
+        start = time.perf_counter()
+        for _ in range(calls):
+            for t, st in zip(layers, streams):
+                with torch.cuda.stream(st):
+                    t.call()
+        torch.cuda.synchronize()
+        ms = (time.perf_counter() - start) / calls * 1e3
+        print("ms", ms, flush=True)
+    assert ms < 5.0
+    for t, w in zip(layers, want):
+        assert torch.equal(t.out[:t.N], w)
